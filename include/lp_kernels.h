@@ -87,6 +87,51 @@ int lpk_attention_bwd_parts(const void* qkv, const void* o, const float* lse, co
 /* The parts that the library chooses (needs no device); 0 for heads that are not 16, 32 or 64 wide. */
 int lpk_attention_parts(int B, int S, int H, int dh, int backward);
 
+/* Linear attention with a decay for each head: with l = exp(log_decay[h]) and a state S [dh, dh] per sequence and head,
+ *   S_t = l S_{t-1} + k_t v_t^T,   o_t = dh^-1/2 q_t S_t      (S_{-1} = s0, zeros if null).
+ * qkv [B*S, 3*H*dh] and o [B*S, H*dh] as in lpk_attention_fwd; log_decay fp32 [H] on the device, 0 or less (a constant: it has no
+ * gradient); states fp32 [B, H, dh, dh].  dh up to 128, B*H up to 65535.  lens (int32 [B] on the device, may be null: all S) are the
+ * sequences' lengths, taken as 0 .. S: positions behind them are neither read nor part of a state, their rows of o and dqkv
+ * become zeros.  s_out (may be null, may be s0) receives the state after the last position.  An infinity or a NaN at a position
+ * reaches the outputs of that one and later ones only.
+ * The backward call takes the same qkv, lens and s0 with the gradients dout of o and ds_out of s_out (may be null: zeros) and
+ * writes dqkv and, where it is not null, the gradient ds0 of s0, which must not overlap ds_out.
+ * scratch_dev: lpk_linear_attention_scratch floats (needs no device; may be 0). */
+int lpk_linear_attention_fwd(int dtype, const void* qkv, const float* log_decay, const int32_t* lens, const float* s0, void* o,
+                             float* s_out, int B, int S, int H, int dh, float* scratch_dev, size_t scratch_elems, void* stream);
+int lpk_linear_attention_bwd(int dtype, const void* qkv, const float* log_decay, const int32_t* lens, const float* s0,
+                             const void* dout, const float* ds_out, void* dqkv, float* ds0, int B, int S, int H, int dh,
+                             float* scratch_dev, size_t scratch_elems, void* stream);
+size_t lpk_linear_attention_scratch(int B, int S, int H, int dh, int backward);
+/* One position more: qkv [B, 3*H*dh], o [B, H*dh], the states are updated in place.  The same as a forward call of S = 1. */
+int lpk_linear_attention_step(int dtype, const void* qkv, const float* log_decay, float* state, void* o, int B, int H, int dh,
+                              void* stream);
+
+/* Dropout of n elements: y = drop(x) (+ res, may be null); y may be x or res.  An element is kept with probability 1 - p (p in
+ * [0, 1], rounded to a multiple of 2^-16) and then divided by the rounded 1 - p.  Which are kept is a function of the element's index,
+ * `site` (a number the caller gives every place of a model that drops) and rng_dev, two 64-bit numbers on the device: a
+ * seed and a step, which the caller changes from step to step, also under a replayed graph.  No mask is stored: the gradient is the
+ * same call on dy, without res.  The generator is Philox4x32-10, counter (index / 8, site, step), key seed; element 8 i + j has the
+ * j-th 16-bit half of the four words, lower half first, and is dropped where that is less than 65536 p.  n up to 2^35. */
+int lpk_dropout(int dtype, const void* x, const void* res, void* y, size_t n, float p, const uint64_t* rng_dev, uint32_t site,
+                void* stream);
+
+/* Root-mean-square norm over the last dimension (d up to 16384) behind a residual branch's dropout and addition:
+ *   r = drop(x) (+ res),  rstd = (mean(r^2) + eps)^-1/2,  y = r rstd g.
+ * res may be null; p, rng_dev and site as in lpk_dropout (index: row * d + column; p 0: nothing is dropped).  r (may be null, may be x
+ * or res) and y (compute dtype, may be null) are outputs, rstd (fp32 [rows], may be null) is kept for the backward call; the norm is
+ * taken of the sum before its rounding to the compute dtype.  y8 (may be null) receives y in 8 bits, e4m3, with one scale for
+ * a row: y8 = y / y8_scale[row], y8_scale = max |y| / 448 (1 for a row of zeros).  At least one of y and y8 is wanted.
+ * Backward, of r as stored (x itself where there was neither res nor dropout): dres = gradient of r (+ add, the stream's own, may be
+ * null), dx = that of x where p > 0 (null where it is not wanted: with p 0 it is dres), dg (+)= sum over rows (may be null).  dres and
+ * dx may be dy, r or add.  scratch_dev: lpk_rmsnorm_scratch floats where dg is wanted (needs no device). */
+int lpk_rmsnorm_fwd(int dtype, const void* x, const void* res, const float* g, void* r, void* y, void* y8, float* y8_scale,
+                    float* rstd, int rows, int d, float eps, float p, const uint64_t* rng_dev, uint32_t site, void* stream);
+int lpk_rmsnorm_bwd(int dtype, const void* dy, const void* r, const float* rstd, const float* g, const void* add, void* dres,
+                    void* dx, float* dg, int rows, int d, int accumulate, float p, const uint64_t* rng_dev, uint32_t site,
+                    float* scratch_dev, size_t scratch_elems, void* stream);
+size_t lpk_rmsnorm_scratch(int rows, int d);
+
 /* LayerNorm over the last dimension (eps 1e-5, biased variance); backward adds `add` to dx if given. */
 int lpk_layernorm_fwd(int dtype, const void* x, const float* g, const float* b, void* y, float* mean, float* rstd,
                       int rows, int d, void* stream);

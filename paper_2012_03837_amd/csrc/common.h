@@ -203,6 +203,22 @@ hipError_t op_attn_fwd(const OpCtx& c, const void* qkv, void* o, float* lse, int
 hipError_t op_attn_bwd(const OpCtx& c, const void* qkv, const void* o, const float* lse, const void* dout,
                        void* dqkv, float* delta, int B, int S, int H, int dh, int causal);
 
+// Linear attention (kernels_linear_attn.hip); states fp32 [B, H, dh, dh], c.partial holds linear_attn_scratch floats.
+size_t linear_attn_scratch(int B, int S, int H, int dh, bool backward);
+hipError_t op_linear_attn_fwd(const OpCtx& c, const void* qkv, const float* log_decay, const int32_t* lens, const float* s0, void* o,
+                              float* s_out, int B, int S, int H, int dh);
+hipError_t op_linear_attn_bwd(const OpCtx& c, const void* qkv, const float* log_decay, const int32_t* lens, const float* s0,
+                              const void* dout, const float* ds_out, void* dqkv, float* ds0, int B, int S, int H, int dh);
+hipError_t op_linear_attn_step(const OpCtx& c, const void* qkv, const float* log_decay, float* state, void* o, int B, int H, int dh);
+
+// Dropout and the residual RMS norm (kernels_rmsnorm.hip); p 0: nothing is dropped and rng (device: seed, step) not read.
+hipError_t op_dropout(const OpCtx& c, const void* x, const void* res, void* y, size_t n, float p, const void* rng, unsigned site);
+size_t rmsnorm_scratch(int rows, int d);
+hipError_t op_rmsnorm_fwd(const OpCtx& c, const void* x, const void* res, const float* g, void* r, void* y, void* y8, float* y8_scale,
+                          float* rstd, int rows, int d, float eps, float p, const void* rng, unsigned site);
+hipError_t op_rmsnorm_bwd(const OpCtx& c, const void* dy, const void* r, const float* rstd, const float* g, const void* add, void* dres,
+                          void* dx, float* dg, int rows, int d, int accumulate, float p, const void* rng, unsigned site);
+
 // Row-wise softmax cross-entropy over logits z [rows, n] (compute dtype, leading dim ld).
 // loss_rows[r] = logsumexp(z_r) - z[r, y_r].  If write_grad: z is overwritten by
 // (softmax(z_r) - onehot(y_r)) * inv_rows, and columns n .. pad_to - 1 (pad_to <= ld; 0: none) by zeros.

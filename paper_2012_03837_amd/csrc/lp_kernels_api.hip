@@ -134,6 +134,41 @@ extern "C" int lpk_attention_bwd_parts(const void* qkv, const void* o, const flo
 extern "C" int lpk_attention_parts(int B, int S, int H, int dh, int backward) {
   return attn_mfma_ok(dh) && B > 0 && S > 0 && H > 0 ? attn_parts(B, S, H, dh, backward != 0) : 0;
 }
+static bool dtype_ok(int dtype) { return dtype == F32 || dtype == BF16; }
+extern "C" int lpk_linear_attention_fwd(int dtype, const void* qkv, const float* log_decay, const int32_t* lens, const float* s0, void* o,
+                                        float* s_out, int B, int S, int H, int dh, float* scratch, size_t scratch_elems, void* stream) {
+  return (int)op_linear_attn_fwd(mk(dtype, stream, scratch, scratch_elems), qkv, log_decay, lens, s0, o, s_out, B, S, H, dh);
+}
+extern "C" int lpk_linear_attention_bwd(int dtype, const void* qkv, const float* log_decay, const int32_t* lens, const float* s0,
+                                        const void* dout, const float* ds_out, void* dqkv, float* ds0, int B, int S, int H, int dh,
+                                        float* scratch, size_t scratch_elems, void* stream) {
+  return (int)op_linear_attn_bwd(mk(dtype, stream, scratch, scratch_elems), qkv, log_decay, lens, s0, dout, ds_out, dqkv, ds0, B, S, H, dh);
+}
+extern "C" size_t lpk_linear_attention_scratch(int B, int S, int H, int dh, int backward) {
+  return linear_attn_scratch(B, S, H, dh, backward != 0);
+}
+extern "C" int lpk_linear_attention_step(int dtype, const void* qkv, const float* log_decay, float* state, void* o, int B, int H, int dh,
+                                         void* stream) {
+  return (int)op_linear_attn_step(mk(dtype, stream), qkv, log_decay, state, o, B, H, dh);
+}
+extern "C" int lpk_dropout(int dtype, const void* x, const void* res, void* y, size_t n, float p, const uint64_t* rng, uint32_t site,
+                           void* stream) {
+  if (!dtype_ok(dtype)) return (int)hipErrorInvalidValue;
+  return (int)op_dropout(mk(dtype, stream), x, res, y, n, p, rng, site);
+}
+extern "C" int lpk_rmsnorm_fwd(int dtype, const void* x, const void* res, const float* g, void* r, void* y, void* y8, float* y8_scale,
+                               float* rstd, int rows, int d, float eps, float p, const uint64_t* rng, uint32_t site, void* stream) {
+  if (!dtype_ok(dtype)) return (int)hipErrorInvalidValue;
+  return (int)op_rmsnorm_fwd(mk(dtype, stream), x, res, g, r, y, y8, y8_scale, rstd, rows, d, eps, p, rng, site);
+}
+extern "C" int lpk_rmsnorm_bwd(int dtype, const void* dy, const void* r, const float* rstd, const float* g, const void* add, void* dres,
+                               void* dx, float* dg, int rows, int d, int accumulate, float p, const uint64_t* rng, uint32_t site,
+                               float* scratch, size_t scratch_elems, void* stream) {
+  if (!dtype_ok(dtype)) return (int)hipErrorInvalidValue;
+  return (int)op_rmsnorm_bwd(mk(dtype, stream, scratch, scratch_elems), dy, r, rstd, g, add, dres, dx, dg, rows, d, accumulate, p, rng, site);
+}
+extern "C" size_t lpk_rmsnorm_scratch(int rows, int d) { return rmsnorm_scratch(rows, d); }
+
 extern "C" int lpk_layernorm_fwd(int dtype, const void* x, const float* g, const float* b, void* y, float* mean,
                                  float* rstd, int rows, int d, void* stream) {
   return (int)op_layernorm_fwd(mk(dtype, stream), x, g, b, y, mean, rstd, rows, d);

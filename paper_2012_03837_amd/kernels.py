@@ -95,6 +95,88 @@ def lpk_attention_parts(B, S, H, dh, backward):
     return lib().lpk_attention_parts(_i(B), _i(S), _i(H), _i(dh), _i(backward))
 
 
+# Entry points that serving calls once a token and layer: their argument types are declared once, and plain numbers go in as they are.
+_vp, _u32 = C.c_void_p, C.c_uint32
+_TYPES = {
+    "lpk_linear_attention_fwd": (_i, [_i] + [_vp] * 6 + [_i] * 4 + [_vp, _sz, _vp]),
+    "lpk_linear_attention_bwd": (_i, [_i] + [_vp] * 8 + [_i] * 4 + [_vp, _sz, _vp]),
+    "lpk_linear_attention_scratch": (_sz, [_i] * 5),
+    "lpk_linear_attention_step": (_i, [_i] + [_vp] * 4 + [_i] * 3 + [_vp]),
+    "lpk_dropout": (_i, [_i] + [_vp] * 3 + [_sz, _f, _vp, _u32, _vp]),
+    "lpk_rmsnorm_fwd": (_i, [_i] + [_vp] * 8 + [_i, _i, _f, _f, _vp, _u32, _vp]),
+    "lpk_rmsnorm_bwd": (_i, [_i] + [_vp] * 8 + [_i] * 3 + [_f, _vp, _u32, _vp, _sz, _vp]),
+    "lpk_rmsnorm_scratch": (_sz, [_i] * 2),
+}
+_entry = {}
+
+
+def _fn(name):
+    f = _entry.get(name)
+    if f is None:
+        f = _entry[name] = C.CFUNCTYPE(_TYPES[name][0], *_TYPES[name][1])((name, lib()))
+    return f
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _run(name, where, *args):
+    """Calls entry point `name`, its last argument the current stream of the device that tensor `where` is on."""
+    import torch
+    dev = where.device
+    if dev.type != "cuda":
+        raise KernelError(f"{name}: tensors on {dev}")
+    if dev.index == torch.cuda.current_device():
+        _ck(_fn(name)(*args, torch.cuda.current_stream().cuda_stream), name)
+    else:
+        with torch.cuda.device(dev):
+            _ck(_fn(name)(*args, torch.cuda.current_stream().cuda_stream), name)
+
+
+def _size(t):
+    return 0 if t is None else t.numel()
+
+
+def lpk_linear_attention_scratch(B, S, H, dh, backward):
+    """Floats of workspace; needs no device."""
+    return _fn("lpk_linear_attention_scratch")(B, S, H, dh, backward)
+
+
+def lpk_linear_attention_fwd(dtype, qkv, log_decay, lens, s0, o, s_out, B, S, H, dh, scratch=None):
+    _run("lpk_linear_attention_fwd", qkv, dtype, _at(qkv), _at(log_decay), _at(lens), _at(s0), _at(o), _at(s_out), B, S, H, dh,
+         _at(scratch), _size(scratch))
+
+
+def lpk_linear_attention_bwd(dtype, qkv, log_decay, lens, s0, dout, ds_out, dqkv, ds0, B, S, H, dh, scratch=None):
+    _run("lpk_linear_attention_bwd", qkv, dtype, _at(qkv), _at(log_decay), _at(lens), _at(s0), _at(dout), _at(ds_out), _at(dqkv),
+         _at(ds0), B, S, H, dh, _at(scratch), _size(scratch))
+
+
+def lpk_linear_attention_step(dtype, qkv, log_decay, state, o, B, H, dh):
+    _run("lpk_linear_attention_step", qkv, dtype, _at(qkv), _at(log_decay), _at(state), _at(o), B, H, dh)
+
+
+def lpk_dropout(dtype, x, res, y, p, rng, site):
+    """rng: two 64-bit integers (seed, step) on the device."""
+    _run("lpk_dropout", x, dtype, _at(x), _at(res), _at(y), x.numel(), p, _at(rng), site)
+
+
+def lpk_rmsnorm_scratch(rows, d):
+    """Floats of workspace; needs no device."""
+    return _fn("lpk_rmsnorm_scratch")(rows, d)
+
+
+def lpk_rmsnorm_fwd(dtype, x, res, g, r, y, y8, y8_scale, rstd, rows, d, eps, p=0.0, rng=None, site=0):
+    _run("lpk_rmsnorm_fwd", x, dtype, _at(x), _at(res), _at(g), _at(r), _at(y), _at(y8), _at(y8_scale), _at(rstd), rows, d, eps, p,
+         _at(rng), site)
+
+
+def lpk_rmsnorm_bwd(dtype, dy, r, rstd, g, add, dres, dx, dg, rows, d, accumulate=0, scratch=None, p=0.0, rng=None, site=0):
+    _run("lpk_rmsnorm_bwd", dy, dtype, _at(dy), _at(r), _at(rstd), _at(g), _at(add), _at(dres), _at(dx), _at(dg), rows, d, accumulate,
+         p, _at(rng), site, _at(scratch), _size(scratch))
+
+
 def lpk_layernorm_fwd(dtype, x, g, b, y, mean, rstd, rows, d):
     _ck(lib().lpk_layernorm_fwd(_i(dtype), _p(x), _p(g), _p(b), _p(y), _p(mean), _p(rstd), _i(rows), _i(d), _stream()),
         "lpk_layernorm_fwd")

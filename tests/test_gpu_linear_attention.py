@@ -1,0 +1,353 @@
+"""Linear attention on the GPU against the oracle's recurrence in 64 bits.
+
+Tolerances (relative 2-norm).  bf16 outputs: one rounding, 2^-8 at most for each value; the operands' parts leave 2^-15 beside it.
+fp32 outputs, the states too: every factor and partial sum is off by 2^-24; a chain of c chunks multiplies a decay c times and
+adds c times, 64 positions are added inside a chunk, and scores are themselves sums over the head: 2^-24 * (4 + sqrt(64) + sqrt(128) +
+c) with c up to 24 here is under 3e-6."""
+import numpy as np
+import pytest
+
+from oracle import ops
+from oracle import residual as R
+
+pytestmark = pytest.mark.gpu
+TOL16, TOL32 = 2.0 ** -8 + 2.0 ** -14, 3e-6
+
+
+@pytest.fixture(scope="module")
+def K():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2012_03837_amd import kernels
+    return kernels
+
+
+def relerr(a, ref):
+    return float(np.linalg.norm((a - ref).ravel()) / max(np.linalg.norm(ref.ravel()), 1e-30))
+
+
+class Case:
+    """Inputs on the host, buffers on the device between guards that no call may touch."""
+
+    def __init__(self, dtype, B, S, H, dh, seed=0, lens=None, states=True, decay=None, shift=0):
+        import torch
+        rng = np.random.default_rng(seed)
+        self.dtype, self.size = dtype, (B, S, H, dh)
+        rnd = lambda *s: (ops.bf16_round(rng.standard_normal(s).astype(np.float32)) if dtype else rng.standard_normal(s)).astype(np.float32)  # noqa: E731
+        self.qkv, self.dout = rnd(B * S, 3 * H * dh), rnd(B * S, H * dh)
+        self.decay = np.asarray(decay if decay is not None else np.log1p(-np.exp2(-np.linspace(1, 9, H))), np.float32)
+        self.lens = None if lens is None else np.asarray(lens, np.int32)
+        self.s0 = rng.standard_normal((B, H, dh, dh)).astype(np.float32) if states else None
+        self.ds_out = rng.standard_normal((B, H, dh, dh)).astype(np.float32) if states else None
+        self.tdt = torch.bfloat16 if dtype else torch.float32
+        self.shift, self.whole = shift, []
+
+    def dev(self, a, dt=None):
+        import torch
+        if a is None:
+            return None
+        t = self.room(a.shape, dt or (torch.int32 if a.dtype == np.int32 else torch.float32), self.shift if dt is not None else 0)
+        t.copy_(torch.from_numpy(np.ascontiguousarray(a)))
+        return t
+
+    def room(self, shape, dt, shift=0, value=0.0):
+        import torch
+        n, pad = int(np.prod(shape)), 64
+        flat = torch.full((n + 2 * pad + shift,), -77 if dt == torch.int32 else -77.0, device="cuda", dtype=dt)
+        t = flat[pad + shift:pad + shift + n]
+        t.fill_(value)
+        self.whole.append((flat, pad + shift, n))
+        return t.view(*shape)
+
+    def guards_stand(self):
+        return all(bool((f[:a] == -77).all()) and bool((f[a + n:] == -77).all()) for f, a, n in self.whole)
+
+    def scratch(self, K, backward):
+        import torch
+        n = K.lpk_linear_attention_scratch(*self.size, backward)
+        return self.room((n,), torch.float32, value=float("nan")) if n else None
+
+    def upload(self):
+        self.d = dict(qkv=self.dev(self.qkv, self.tdt), decay=self.dev(self.decay), lens=self.dev(self.lens), s0=self.dev(self.s0),
+                      dout=self.dev(self.dout, self.tdt), ds_out=self.dev(self.ds_out))
+        return self.d
+
+    def outputs(self):
+        import torch
+        B, S, H, dh = self.size
+        d = self.d
+        d["o"], d["dqkv"] = (self.room((B * S, w * H * dh), self.tdt, self.shift, float("nan")) for w in (1, 3))
+        d["s_out"], d["ds0"] = (self.room((B, H, dh, dh), torch.float32, value=float("nan")) if self.s0 is not None else None for _ in range(2))
+        return d
+
+    def forward(self, K):
+        d = self.d
+        K.lpk_linear_attention_fwd(self.dtype, d["qkv"], d["decay"], d["lens"], d["s0"], d["o"], d["s_out"], *self.size, self.scratch(K, 0))
+
+    def backward(self, K):
+        d = self.d
+        K.lpk_linear_attention_bwd(self.dtype, d["qkv"], d["decay"], d["lens"], d["s0"], d["dout"], d["ds_out"], d["dqkv"], d["ds0"],
+                                   *self.size, self.scratch(K, 1))
+
+    def heads(self, a):
+        B, S, H, dh = self.size
+        return np.asarray(a, np.float64).reshape(B, S, H, dh).transpose(0, 2, 1, 3)
+
+    def reference(self):
+        B, S, H, dh = self.size
+        w = H * dh
+        q, k, v = (self.heads(self.qkv[:, i * w:(i + 1) * w]) for i in range(3))
+        flat = lambda a: a.transpose(0, 2, 1, 3).reshape(B * S, w)  # noqa: E731
+        f64 = lambda a: None if a is None else a.astype(np.float64)  # noqa: E731
+        o, s = R.linear_attention_fwd(q, k, v, f64(self.decay), f64(self.s0), self.lens)
+        dq, dk, dv, ds = R.linear_attention_bwd(q, k, v, f64(self.decay), self.heads(self.dout), f64(self.s0), f64(self.ds_out), self.lens)
+        return dict(o=flat(o), s_out=s, dqkv=np.concatenate([flat(dq), flat(dk), flat(dv)], 1), ds0=ds)
+
+    def check(self, K):
+        import torch
+        self.upload()
+        self.outputs()
+        self.forward(K)
+        self.backward(K)
+        ref = self.reference()
+        w = self.size[2] * self.size[3]
+        tol = TOL16 if self.dtype else TOL32
+        got = {n: None if t is None else t.float().cpu().numpy().astype(np.float64) for n, t in self.d.items() if n in ref}
+        assert relerr(got["o"], ref["o"]) <= tol
+        for i, n in enumerate("qkv"):
+            assert relerr(got["dqkv"][:, i * w:(i + 1) * w], ref["dqkv"][:, i * w:(i + 1) * w]) <= tol, "d" + n
+        if self.s0 is not None:
+            assert relerr(got["s_out"], ref["s_out"]) <= TOL32
+            assert relerr(got["ds0"], ref["ds0"]) <= TOL32
+        if self.lens is not None:                      # rows behind a sequence
+            B, S = self.size[:2]
+            for b in range(B):
+                n = int(np.clip(self.lens[b], 0, S))
+                assert not got["o"].reshape(B, S, -1)[b, n:].any() and not got["dqkv"].reshape(B, S, -1)[b, n:].any()
+        assert self.guards_stand()
+        torch.cuda.synchronize()
+        return got
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("S", [1, 2, 31, 32, 33, 63, 64, 65, 128, 129, 200])
+def test_lengths(K, dtype, S):
+    Case(dtype, 2, S, 3, 64, seed=S).check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("dh", [1, 3, 8, 16, 20, 24, 32, 40, 63, 64, 72, 100, 127, 128])
+def test_head_sizes(K, dtype, dh):
+    Case(dtype, 2, 150, 2, dh, seed=dh).check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("B,S,H,dh", [(1, 1500, 1, 64), (2, 1031, 3, 32), (1, 769, 2, 128), (3, 512, 2, 16)])
+def test_long_axis_in_segments(K, dtype, B, S, H, dh):
+    assert K.lpk_linear_attention_scratch(B, S, H, dh, 0) > 0 and K.lpk_linear_attention_scratch(B, S, H, dh, 1) > 0
+    Case(dtype, B, S, H, dh, seed=B).check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_many_short_sequences_uncut(K, dtype):
+    B, S, H, dh = 130, 140, 8, 32
+    assert K.lpk_linear_attention_scratch(B, S, H, dh, 0) == K.lpk_linear_attention_scratch(B, S, H, dh, 1) == 0
+    Case(dtype, B, S, H, dh).check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("S,dh,lens", [(100, 64, [0, 1, 100, 64]), (700, 64, [0, 700, 129, 65]), (700, 32, [256, 257, -5, 9999]),
+                                       (300, 128, [1, 192, 0, 299])])
+def test_ragged_batches(K, dtype, S, dh, lens):
+    case = Case(dtype, 4, S, 2, dh, seed=S, lens=lens)
+    # what stands behind a sequence is not looked at
+    for a, w in ((case.qkv, 6 * dh), (case.dout, 2 * dh)):
+        x = a.reshape(4, S, w)
+        for b, n in enumerate(np.clip(lens, 0, S)):
+            x[b, n:] = np.nan
+    reference = Case.reference
+
+    def clean(self):
+        kept = self.qkv, self.dout
+        self.qkv, self.dout = (np.nan_to_num(a) for a in kept)
+        out = reference(self)
+        self.qkv, self.dout = kept
+        return out
+    case.reference = clean.__get__(case)
+    case.check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("decay", [[0.0, 0.0], [-np.inf, -50.0], [-1e-4, -4.0]])
+def test_decays_at_their_limits(K, dtype, decay):
+    Case(dtype, 2, 333, 2, 64, seed=5, decay=decay).check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("states", [False, True])
+def test_unaligned_buffers(K, dtype, states):
+    Case(dtype, 2, 300, 2, 64, seed=6, states=states, shift=1).check(K)
+
+
+def test_states_alone(K):
+    """A sequence without positions hands its state through; without states nothing is read or written for them."""
+    import torch
+    case = Case(1, 2, 0, 2, 64)
+    d = case.upload()
+    s_out = case.room((2, 2, 64, 64), torch.float32)
+    K.lpk_linear_attention_fwd(1, None or d["s0"], d["decay"], None, d["s0"], d["s0"], s_out, 2, 0, 2, 64)
+    assert torch.equal(s_out, d["s0"])
+    ds0 = case.room((2, 2, 64, 64), torch.float32)
+    K.lpk_linear_attention_bwd(1, d["s0"], d["decay"], None, d["s0"], d["s0"], d["ds_out"], d["s0"], ds0, 2, 0, 2, 64)
+    assert torch.allclose(ds0, d["ds_out"], rtol=3 * 2.0 ** -24, atol=0)
+    assert case.guards_stand()
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("B,S,dh", [(2, 100, 64), (1, 1000, 64), (1, 300, 128)])
+def test_state_in_place(K, dtype, B, S, dh):
+    import torch
+    case = Case(dtype, B, S, 2, dh, seed=3)
+    d = case.upload()
+    case.outputs()
+    case.forward(K)
+    o, s = d["o"].clone(), d["s_out"].clone()
+    K.lpk_linear_attention_fwd(dtype, d["qkv"], d["decay"], None, d["s0"], d["o"], d["s0"], *case.size, case.scratch(K, 0))
+    assert torch.equal(d["o"], o) and torch.equal(d["s0"], s)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("B,H,dh", [(1, 1, 1), (3, 5, 7), (1, 12, 64), (5, 3, 40), (2, 2, 128), (300, 8, 16), (4, 3, 66)])
+def test_step_is_a_call_of_one_position(K, dtype, B, H, dh):
+    case = Case(dtype, B, 1, H, dh, seed=dh)
+    d = case.upload()
+    case.outputs()
+    K.lpk_linear_attention_step(dtype, d["qkv"], d["decay"], d["s0"], d["o"], B, H, dh)
+    ref = case.reference()
+    assert relerr(d["o"].float().cpu().numpy().astype(np.float64), ref["o"]) <= (TOL16 if dtype else TOL32)
+    assert relerr(d["s0"].cpu().numpy().astype(np.float64), ref["s_out"]) <= TOL32
+    assert case.guards_stand()
+
+
+def test_step_on_an_unaligned_state(K):
+    import torch
+    case = Case(1, 3, 1, 2, 64)
+    d = case.upload()
+    case.outputs()
+    state = case.room((3, 2, 64, 64), torch.float32, shift=1)
+    state.copy_(d["s0"])
+    K.lpk_linear_attention_step(1, d["qkv"], d["decay"], state, d["o"], 3, 2, 64)
+    assert relerr(state.cpu().numpy().astype(np.float64), case.reference()["s_out"]) <= TOL32
+    assert case.guards_stand()
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_prompt_then_tokens(K, dtype):
+    """A prompt in one call and the rest one by one give what one call gives."""
+    B, S, H, dh, cut = 2, 150, 3, 64, 131
+    case = Case(dtype, B, S, H, dh, seed=8)
+    d = case.upload()
+    ref = case.reference()
+    rows = d["qkv"].view(B, S, -1)
+    state = case.room(d["s0"].shape, d["s0"].dtype)
+    o = case.room((B, cut, H * dh), case.tdt)
+    prompt = rows[:, :cut].contiguous()
+    K.lpk_linear_attention_fwd(dtype, prompt, d["decay"], None, d["s0"], o, state, B, cut, H, dh, case.scratch(K, 0))
+    got = [o]
+    for t in range(cut, S):
+        one = case.room((B, 1, H * dh), case.tdt)
+        K.lpk_linear_attention_step(dtype, rows[:, t].contiguous(), d["decay"], state, one, B, H, dh)
+        got.append(one)
+    import torch
+    assert relerr(torch.cat(got, 1).float().cpu().numpy().astype(np.float64).reshape(B * S, -1), ref["o"]) <= (TOL16 if dtype else TOL32)
+    assert relerr(state.cpu().numpy().astype(np.float64), ref["s_out"]) <= TOL32
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("S,dh", [(130, 64), (130, 32), (600, 64), (130, 128)])
+@pytest.mark.parametrize("which,value", [(0, np.nan), (1, np.inf), (2, np.inf), (2, np.nan), (3, -np.inf), (3, np.nan)])
+def test_infinities_reach_no_position_they_must_not(K, dtype, S, dh, which, value):
+    """q, k, v or dout with one bad row: forward outputs before it, and gradients that do not depend on it, are those of the clean run."""
+    at, H = 77, 2
+    runs = []
+    for bad in (False, True):
+        case = Case(dtype, 1, S, H, dh, seed=4)
+        if bad:
+            (case.dout if which == 3 else case.qkv)[at, (0 if which == 3 else which * H * dh) + 5] = value       # head 0
+        d = case.upload()
+        case.outputs()
+        case.forward(K)
+        case.backward(K)
+        runs.append({n: d[n].float().cpu().numpy() for n in ("o", "dqkv")})
+    clean, got = runs
+    w = H * dh
+    cols = {"o": clean["o"], **{n: clean["dqkv"][:, i * w:(i + 1) * w] for i, n in enumerate(("dq", "dk", "dv"))}}
+    outs = {"o": got["o"], **{n: got["dqkv"][:, i * w:(i + 1) * w] for i, n in enumerate(("dq", "dk", "dv"))}}
+    # positions of head 0 that depend on the row
+    after, until, only, none = range(at, S), range(0, at + 1), [at], []
+    touched = [dict(o=only, dq=none, dk=until, dv=until), dict(o=after, dq=after, dk=none, dv=until),
+               dict(o=after, dq=after, dk=until, dv=none), dict(o=none, dq=only, dk=until, dv=until)][which]
+    # a step of the tile products may be taken in another order where a chunk holds such a value: one rounding more
+    tol = 2.0 ** -7 if dtype else 1e-5
+    for n in outs:
+        rows = np.ones(S, bool)
+        rows[list(touched[n])] = False
+        if rows.any():
+            assert np.isfinite(outs[n][rows]).all(), n
+            assert relerr(outs[n][rows].astype(np.float64), cols[n][rows].astype(np.float64)) <= tol, n
+        assert relerr(outs[n][:, dh:].astype(np.float64), cols[n][:, dh:].astype(np.float64)) <= tol, n        # the other head
+    assert not np.isfinite(outs["dv" if which in (0, 1, 3) else "dk"][at, :dh]).all()
+
+
+@pytest.mark.parametrize("B,S,H,dh", [(2, 300, 2, 64), (1, 1200, 2, 64)])
+def test_runs_are_identical_bit_for_bit_and_replay(K, B, S, H, dh):
+    """Two eager runs, and a captured pair of calls that is replayed with other inputs between eager work."""
+    import torch
+    case = Case(1, B, S, H, dh, seed=9)
+    d = case.upload()
+    case.outputs()
+    ws = [case.scratch(K, 0), case.scratch(K, 1)]
+
+    def run():
+        K.lpk_linear_attention_fwd(1, d["qkv"], d["decay"], None, d["s0"], d["o"], d["s_out"], *case.size, ws[0])
+        K.lpk_linear_attention_bwd(1, d["qkv"], d["decay"], None, d["s0"], d["dout"], d["ds_out"], d["dqkv"], d["ds0"], *case.size, ws[1])
+    names = ("o", "s_out", "dqkv", "ds0")
+    run()
+    first = {n: d[n].clone() for n in names}
+    run()
+    assert all(torch.equal(first[n], d[n]) for n in names)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        run()
+    clean = d["qkv"].clone()
+    for i in range(3):
+        d["qkv"].copy_(clean * (1.0 + 0.5 * i))
+        for n in names:
+            d[n].fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {n: d[n].clone() for n in names}
+        run()
+        assert all(torch.equal(got[n], d[n]) for n in names), i
+
+
+def test_two_streams_at_once(K):
+    import torch
+    cases = [Case(1, 1, 900, 2, 64, seed=i) for i in range(2)]
+    for c in cases:
+        c.upload()
+        c.outputs()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, s in zip(cases, (torch.cuda.Stream(), torch.cuda.Stream())):
+            with torch.cuda.stream(s):
+                c.forward(K)
+                c.backward(K)
+    torch.cuda.synchronize()
+    for c in cases:
+        ref = c.reference()
+        for n in ("o", "dqkv"):
+            assert relerr(c.d[n].float().cpu().numpy().astype(np.float64), ref[n]) <= TOL16

@@ -1,0 +1,76 @@
+"""What the residual chain's entry points refuse, on the host: every call here ends before anything is launched (the addresses are
+not memory)."""
+import ctypes as C
+
+import pytest
+
+P, NULL = 1 << 20, None            # never read
+NAN = float("nan")
+
+
+@pytest.fixture(scope="module")
+def K():
+    from paper_2012_03837_amd import kernels
+    return kernels
+
+
+def call(K, name, **kw):
+    args = DEFAULTS[name] | kw
+    assert set(args) == set(DEFAULTS[name])
+    return K._fn(name)(*args.values(), None)
+
+
+SHAPE = dict(B=2, S=640, H=3, dh=64)
+DEFAULTS = {
+    "lpk_linear_attention_fwd": dict(dtype=1, qkv=P, log_decay=P, lens=P, s0=P, o=P, s_out=P, **SHAPE, scratch=P, elems=1 << 30),
+    "lpk_linear_attention_bwd": dict(dtype=1, qkv=P, log_decay=P, lens=P, s0=P, dout=P, ds_out=P, dqkv=P, ds0=P, **SHAPE, scratch=P,
+                                     elems=1 << 30),
+    "lpk_linear_attention_step": dict(dtype=1, qkv=P, log_decay=P, state=P, o=P, B=2, H=3, dh=64),
+    "lpk_dropout": dict(dtype=1, x=P, res=P, y=P, n=100, p=0.1, rng=P, site=0),
+    "lpk_rmsnorm_fwd": dict(dtype=1, x=P, res=P, g=P, r=P, y=P, y8=P, y8_scale=P, rstd=P, rows=4, d=64, eps=1e-5, p=0.1, rng=P, site=0),
+    "lpk_rmsnorm_bwd": dict(dtype=1, dy=P, r=P, rstd=P, g=P, add=P, dres=P, dx=P, dg=P, rows=4, d=64, accumulate=0, p=0.1, rng=P, site=0,
+                            scratch=P, elems=1 << 20),
+}
+SHAPES = [dict(dtype=2), dict(dtype=-1), dict(dh=0), dict(dh=129), dict(H=0), dict(B=-1), dict(log_decay=NULL), dict(qkv=NULL)]
+BAD = {
+    "lpk_linear_attention_fwd": SHAPES + [dict(S=-1), dict(o=NULL), dict(scratch=NULL), dict(elems=1), dict(B=65536, H=1), dict(H=1 << 30)],
+    "lpk_linear_attention_bwd": SHAPES + [dict(S=-1), dict(dqkv=NULL), dict(dout=NULL), dict(scratch=NULL), dict(elems=1),
+                                          dict(B=1 << 15, H=3)],
+    "lpk_linear_attention_step": SHAPES + [dict(state=NULL), dict(o=NULL), dict(B=1 << 30, H=3), dict(H=1 << 30)],
+    "lpk_dropout": [dict(dtype=2), dict(p=-0.1), dict(p=1.1), dict(p=NAN), dict(rng=NULL), dict(rng=P + 4), dict(x=NULL), dict(y=NULL),
+                    dict(n=(1 << 35) + 1)],
+    "lpk_rmsnorm_fwd": [dict(dtype=2), dict(rows=-1), dict(d=0), dict(d=16385), dict(p=-0.1), dict(p=1.1), dict(p=NAN), dict(rng=NULL),
+                        dict(rng=P + 4), dict(x=NULL), dict(g=NULL), dict(y=NULL, y8=NULL), dict(y8_scale=NULL),
+                        dict(rows=1 << 30, d=64)],
+    "lpk_rmsnorm_bwd": [dict(dtype=2), dict(rows=-1), dict(d=0), dict(d=16385), dict(p=-0.1), dict(p=NAN), dict(rng=NULL), dict(dy=NULL),
+                        dict(r=NULL), dict(rstd=NULL), dict(g=NULL), dict(dres=NULL, dx=NULL, dg=NULL), dict(scratch=NULL), dict(elems=1),
+                        dict(rows=1 << 30, d=64)],
+}
+
+
+@pytest.mark.parametrize("name,kw", [(n, kw) for n in BAD for kw in BAD[n]], ids=str)
+def test_refused(K, name, kw):
+    assert call(K, name, **kw) == 1          # hipErrorInvalidValue
+
+
+@pytest.mark.parametrize("name,kw", [
+    ("lpk_linear_attention_fwd", dict(B=0)), ("lpk_linear_attention_bwd", dict(B=0)), ("lpk_linear_attention_step", dict(B=0)),
+    ("lpk_dropout", dict(n=0)), ("lpk_rmsnorm_fwd", dict(rows=0)), ("lpk_rmsnorm_bwd", dict(rows=0, dg=NULL))], ids=str)
+def test_nothing_to_do(K, name, kw):
+    assert call(K, name, **kw) == 0
+
+
+def test_workspace_sizes(K):
+    assert K.lpk_linear_attention_scratch(1, 64, 4, 64, 0) == 0                     # one chunk: nothing to cut
+    assert K.lpk_linear_attention_scratch(1024, 4096, 16, 64, 1) == 0               # enough sequences and heads
+    n = K.lpk_linear_attention_scratch(1, 4096, 2, 64, 0)
+    assert n > 0 and n % (2 * 64 * 64) == 0
+    assert K.lpk_linear_attention_scratch(1, 4096, 2, 200, 0) == 0                  # a head that no call takes
+    assert K.lpk_rmsnorm_scratch(8192, 768) >= 768 and K.lpk_rmsnorm_scratch(1, 5) >= 5
+
+
+def test_wrappers_want_device_tensors(K):
+    import torch
+    x = torch.zeros(8)
+    with pytest.raises(K.KernelError):
+        K.lpk_dropout(0, x, None, x, 0.0, None, 0)
