@@ -1,8 +1,8 @@
 // Linear attention with a decay for each head.  With l = exp(log_decay[h]) and the state S [dh, dh] in fp32,
 //   S_t = l S_{t-1} + k_t v_t^T,   o_t = dh^-1/2 q_t S_t   (position t included).
-// Chunks of 64 positions: with X the state before a chunk, u = 0 .. 63 the position in it and e = 1,
+// Chunks of 32 positions: with X the state before a chunk, u = 0 .. 31 the position in it and e = 1,
 //   O = dh^-1/2 ( ((Q K^T) . D) V + diag(l^{u + e}) Q X ),  D[u, w] = l^{u - w} for w <= u, otherwise 0,
-//   X' = l^c X + sum_u l^{c - u - e} k_u v_u^T              (c: positions of the chunk, 64 but for the last).
+//   X' = l^c X + sum_u l^{c - u - e} k_u v_u^T              (c: positions of the chunk, 32 but for the last).
 // The gradients are the same map of other operands, so that one kernel serves both directions:
 //   dQ = map(q <- dO, k <- V, v <- K),
 //   dV = map(q <- K, k <- Q, v <- dO) and dK = map(q <- V, k <- dO, v <- Q) with the positions taken from the last to the first
@@ -10,9 +10,13 @@
 // A long axis over few heads is cut into segments of whole chunks: k_linear_states leaves what each adds to the state,
 // k_linear_scan turns that into the state before each, and the blocks of k_linear_walk go over their segments side by side.
 //
-// Products run on the matrix cores, 32 x 32 tiles; as in the softmax kernels the score tile is kept transposed, because the
-// accumulators of K Q^T are the operand layout of the product behind it.  The state lives in fp32 accumulators, a 32 x 32 tile of it in
-// each wave.  Whatever has more bits than the compute dtype (scores times decay, keys times decay, the state as an operand) is
+// Products run on the matrix cores, 32 x 32 tiles.  A wave keeps 32 columns of the state, all rows of them, in fp32 accumulators, and
+// the waves of a head share the chunk's q, k and v through LDS.  The accumulators' layout is that of an operand whose reduction
+// index is the row, so that the state and the scores K Q^T go from one product to the next without leaving the registers.
+// Heads of up to 64: two waves for every 32 columns, one with the state, which multiplies it with the chunk's queries and then
+// adds the chunk to it, and one with the chunk's own scores and their product with the values, which adds both parts of the output.
+// Wider heads, whose state fills the registers anyway: one wave does both.
+// Whatever has more bits than the compute dtype (scores times decay, values times decay, the state as an operand) is
 // split into two bf16 parts (three where the state itself is an output): the parts' products are exact and summed in fp32.  With one part
 // alone every such rounding adds an error as large as that of the rounded output.
 #include "common.h"
@@ -22,7 +26,7 @@ namespace lp {
 
 namespace {
 
-constexpr int kChunk = 64;
+constexpr int kChunk = 32;
 constexpr float kLog2e = 1.4426950408889634f;
 typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
@@ -39,16 +43,19 @@ __device__ __forceinline__ f32x16 mma(const f32x8& a, const f32x8& b, f32x16 c) 
   for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
   return c;
 }
-__device__ __forceinline__ bf16x8 frag_row(const bf16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
-__device__ __forceinline__ f32x8 frag_row(const float* p) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-  f32x8 r;
+// Operand whose reduction index is the column of an LDS tile: eight of sixteen columns, at 4 hf + {0..3} and 8 + 4 hf + {0..3}, the order
+// of an accumulator's values; p points at the row's column 4 hf.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::V frag_row(const T* p) {
+  typedef __attribute__((ext_vector_type(4))) T T4;
+  const T4 a = *reinterpret_cast<const T4*>(p), b = *reinterpret_cast<const T4*>(p + 8);
+  typename Frag<T>::V r;
 #pragma unroll
   for (int e = 0; e < 4; ++e) { r[e] = a[e]; r[4 + e] = b[e]; }
   return r;
 }
 // Operand whose reduction index is the row of an LDS tile: lane (n, hf) gets column c0 + n of rows r0 + 4 hf + {0..3} and
-// r0 + 8 + 4 hf + {0..3}, the order of an accumulator's values; bf16 by the transposing read (its 16-lane groups: lane 4 r + c
+// r0 + 8 + 4 hf + {0..3}; bf16 by the transposing read (its 16-lane groups: lane 4 r + c
 // supplies four columns 4 c .. of row r and lane 4 c + e receives column 4 c + e of the four rows).
 template <int LD>
 __device__ __forceinline__ bf16x8 frag_col(const bf16_t (*s)[LD], int r0, int c0, int lane) {
@@ -69,15 +76,26 @@ __device__ __forceinline__ f32x8 frag_col(const float (*s)[LD], int r0, int c0, 
   for (int e = 0; e < 8; ++e) r[e] = s[r0 + 8 * (e / 4) + 4 * hf + e % 4][c0 + n];
   return r;
 }
-// fp32 values as NP operands whose sum they are (to 2^-8 NP); one where the compute dtype is fp32.
+// fp32 values as NP operands whose sum they are (to 2^-9 NP); one where the compute dtype is fp32.  By twos: a conversion rounds a
+// pair, and the pair's rounded values are its two halves in place.
 template <int NP>
 __device__ __forceinline__ void split(const f32x8& v, bf16x8 (&f)[NP]) {
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+  u32x4 w[NP];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float r = v[e];
+  for (int e = 0; e < 4; ++e) {
+    f32x2 r = {v[2 * e], v[2 * e + 1]};
 #pragma unroll
-    for (int s = 0; s < NP; ++s) { f[s][e] = (bf16_t)r; r -= (float)f[s][e]; }
+    for (int s = 0; s < NP; ++s) {
+      const unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector(r, bf16x2));
+      w[s][e] = h;
+      r[0] -= __builtin_bit_cast(float, h << 16);
+      r[1] -= __builtin_bit_cast(float, h & 0xffff0000u);
+    }
   }
+#pragma unroll
+  for (int s = 0; s < NP; ++s) f[s] = __builtin_bit_cast(bf16x8, w[s]);
 }
 __device__ __forceinline__ void split(const f32x8& v, f32x8 (&f)[1]) { f[0] = v; }
 template <typename V, int NP>
@@ -85,6 +103,23 @@ __device__ __forceinline__ f32x16 mma_parts(const V (&a)[NP], const V& b, f32x16
 #pragma unroll
   for (int s = NP - 1; s >= 0; --s) c = mma(a[s], b, c);
   return c;
+}
+template <typename V, int NP>
+__device__ __forceinline__ f32x16 mma_parts(const V& a, const V (&b)[NP], f32x16 c) {
+#pragma unroll
+  for (int s = NP - 1; s >= 0; --s) c = mma(a, b[s], c);
+  return c;
+}
+template <int NP>
+__device__ __forceinline__ void split_half(const f32x16& v, int kk, bf16x8 (&f)[NP]) {     // values 8 kk .. of an accumulator
+  f32x8 t;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) t[e] = v[8 * kk + e];
+  split(t, f);
+}
+__device__ __forceinline__ void split_half(const f32x16& v, int kk, f32x8 (&f)[1]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[0][e] = v[8 * kk + e];
 }
 __device__ __forceinline__ void zero(f32x16& a) {
 #pragma unroll
@@ -97,49 +132,64 @@ __device__ __forceinline__ float decay_of(const float* log_decay, int h) {
   return (g < -1e4f ? -1e4f : g) * kLog2e;
 }
 
-template <typename T> constexpr int kPerChunk = 16 / (int)sizeof(T);     // elements of a 16-byte load
-
-// [64 rows][W columns] of a matrix on the way into LDS, in registers while the chunk before it is computed.  Rows from `rows`
-// on and columns from `cols` on are zeros (and not read).  VEC: rows are whole 16-byte chunks on 16-byte boundaries.
-template <typename T, int W, int NT, bool VEC>
+// [R rows][W columns] of a matrix on the way into LDS, in registers while the chunk before it is computed, by a block of NT
+// threads.  Rows past the sequence repeat its last one (they meet scores that are left out, weights of 0 and
+// outputs that are not stored) and columns past `cols` are zeros.  VEC: rows are whole 16-byte loads on 16-byte boundaries.
+template <typename T, int W, int R, int NT, bool VEC>
 struct TileRegs {
-  static constexpr int E = kPerChunk<T>, CPR = W / E, N = (kChunk * CPR + NT - 1) / NT;
-  static_assert(kChunk * CPR % NT == 0, "whole loads");
+  static constexpr int E = 16 / (int)sizeof(T), CPR = W / E, N = R * CPR / NT;
+  static_assert(R * CPR % NT == 0, "whole loads");
   typedef __attribute__((ext_vector_type(E))) T V;
   V v[N];
-  __device__ __forceinline__ void load(const T* p, ptrdiff_t ld, int rows, int cols) {
+  unsigned off[N];             // bytes behind the chunk's lowest row
+  // rows of a chunk with `count` positions; back: position 0 is the highest row
+  __device__ __forceinline__ void rows(int ld, bool back, int count, int cols) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int x = threadIdx.x + NT * i, r = x / CPR, c = x % CPR * E;
+      const int rr = r < count ? r : count - 1, m = back ? count - 1 - rr : rr;
+      off[i] = (__umul24(m, ld) + (c < cols ? c : 0)) * (unsigned)sizeof(T);
+    }
+  }
+  __device__ __forceinline__ void load(const T* low, int cols) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[i][e] = (T)0.f;
-      if (r < rows) {
-        const T* q = p + (ptrdiff_t)r * ld + c;
-        if (VEC) {
-          if (c < cols) v[i] = *reinterpret_cast<const V*>(q);
-        } else {
+    for (int i = 0; i < N; ++i) {
+      const char* p = reinterpret_cast<const char*>(low) + off[i];
+      if (VEC) {
+        v[i] = *reinterpret_cast<const V*>(p);
+      } else {
+        const int c = (threadIdx.x + NT * i) % CPR * E;
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (c + e < cols) v[i][e] = q[e];
-        }
+        for (int e = 0; e < E; ++e) v[i][e] = reinterpret_cast<const T*>(p)[c + e < cols ? e : 0];
       }
     }
   }
   template <int LD>
-  __device__ __forceinline__ void store(T (*s)[LD]) const {
+  __device__ __forceinline__ void store(T (*s)[LD], int cols) {
+    if (cols < W) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[i][e] = (threadIdx.x + NT * i) % CPR * E + e < cols ? v[i][e] : (T)0.f;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int x = threadIdx.x + NT * i;
       *reinterpret_cast<V*>(&s[x / CPR][x % CPR * E]) = v[i];
     }
   }
+  // whether one is an infinity or a NaN
   __device__ __forceinline__ bool non_finite() const {
-    bool bad = false;
+    typedef __attribute__((ext_vector_type(4))) unsigned U;
+    // without its sign and one exponent step up, such a number (and no other) has the sign's bit set
+    constexpr unsigned size = sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu, step = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
+    unsigned bad = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int e = 0; e < E; ++e) bad = bad || !(__builtin_fabsf((float)v[i][e]) < INFINITY);
-    return bad;
+    for (int i = 0; i < N; ++i) {
+      const U w = (__builtin_bit_cast(U, v[i]) & size) + step;
+      bad |= w[0] | w[1] | w[2] | w[3];
+    }
+    return (bad & ~size) != 0;
   }
 };
 
@@ -147,7 +197,7 @@ struct TileRegs {
 struct LinearJob {
   const void *q, *k, *v;
   void* out;
-  int64_t ldq, ldk, ldv, ldo;      // elements
+  int ldq, ldk, ldv, ldo;          // elements
   const float* init;               // state that came in ([B, H, dh, dh], null: zeros), times in_scale, transposed if `turned`
   float* fin;                      // state that goes out, times out_scale (null: not wanted)
   const float* before;             // states before the segments ([B H, segments, dh, dh]), transposed if `turned`
@@ -168,208 +218,217 @@ struct LinearShape {
   }
 };
 
-// The state's tiles: wave w holds rows 32 (w & 1) (and + 64) and columns 32 (w >> 1).
-template <int DK> constexpr int kTiles = DK == 128 ? 2 : 1;
+// What a block works on: its job, sequence, head and stretch of positions.
+struct Place {
+  int job, seg, bh, h, len, first, last, stop, units;
+  size_t row0, row;            // the sequence's first row; the row of position 0 in the job's direction
+  float g2;
+};
+// Blocks go to the eight dies by turns of their number, x first: the jobs (y) of one segment, which share its rows, run on one die.
+__device__ __forceinline__ bool place(const LinearShape& sh, int units, Place& p) {
+  const unsigned unit = blockIdx.z * 8 + blockIdx.x;
+  p.job = blockIdx.y;
+  if (unit >= (unsigned)units) return false;
+  const unsigned bh = sh.segments > 1 ? unit / (unsigned)sh.segments : unit, b = bh / (unsigned)sh.H;
+  p.bh = bh;
+  p.seg = unit - bh * sh.segments;
+  p.h = bh - b * sh.H;
+  p.len = sh.length(b);
+  p.first = p.seg * sh.per * kChunk;
+  p.last = p.first + sh.per * kChunk < sh.S ? p.first + sh.per * kChunk : sh.S;       // padding included
+  p.stop = p.last < p.len ? p.last : p.len;
+  p.row0 = (size_t)b * sh.S;
+  p.g2 = decay_of(sh.log_decay, p.h);
+  return true;
+}
+template <typename T>
+__device__ __forceinline__ const T* column(const void* m, size_t row, int ld, int h, int dh) {
+  return (const T*)m + (row * ld + (size_t)h * dh);
+}
+// Lowest row of the chunk of `count` positions from u0 on.
+template <typename T>
+__device__ __forceinline__ const T* lowest(const T* p, int ld, bool back, int u0, int count) {
+  return p + (ptrdiff_t)(back ? -(u0 + count - 1) : u0) * ld;
+}
+__device__ __forceinline__ int acc_row(int v, int hf) { return 8 * (v / 4) + 4 * hf + v % 4; }      // of an accumulator's value
 
-// acc += sum over the chunk's positions of weight * k v^T, for the wave's tiles.
-template <typename T, int DK, int NP, int LDK, int LDV>
-__device__ __forceinline__ void add_outer(f32x16 (&state)[kTiles<DK>], const T (*ks)[LDK], const T (*vs)[LDV], const float* weight, int ib,
-                                          int jb, int lane) {
+// state += sum over the chunk's positions of k (weight v)^T: all rows, columns 32 col ..
+template <typename T, int DK, int NP, int LD>
+__device__ __forceinline__ void add_outer(f32x16 (&state)[DK / 32], const T (*ks)[LD], const T (*vs)[LD], const float* weight, int col, int lane) {
   const int hf = lane >> 5;
 #pragma unroll
-  for (int kk = 0; kk < 4; ++kk) {
-    const typename Frag<T>::V b = frag_col<LDV>(vs, 16 * kk, 32 * jb, lane);
+  for (int kk = 0; kk < 2; ++kk) {
+    const typename Frag<T>::V v = frag_col<LD>(vs, 16 * kk, 32 * col, lane);
     f32x8 w;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const f32x4 t = *reinterpret_cast<const f32x4*>(weight + 16 * kk + 8 * x + 4 * hf);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[4 * x + e] = t[e];
+      for (int e = 0; e < 4; ++e) w[4 * x + e] = (float)v[4 * x + e] * t[e];
     }
+    typename Frag<T>::V f[NP];
+    split(w, f);
 #pragma unroll
-    for (int i = 0; i < kTiles<DK>; ++i) {
-      const typename Frag<T>::V a = frag_col<LDK>(ks, 16 * kk, 32 * ib + 64 * i, lane);
-      f32x8 p;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = (float)a[e] * w[e];
-      typename Frag<T>::V f[NP];
-      split(p, f);
-      state[i] = mma_parts(f, b, state[i]);
-    }
+    for (int i = 0; i < DK / 32; ++i) state[i] = mma_parts(frag_col<LD>(ks, 16 * kk, 32 * i, lane), f, state[i]);
   }
 }
+template <int ND>
+__device__ __forceinline__ void scale(f32x16 (&state)[ND], float by) {
+#pragma unroll
+  for (int i = 0; i < ND; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) state[i][v] *= by;
+}
 
-template <typename T, int DK, int DV, int NP>
+template <typename T> constexpr int kPad = 16 / (int)sizeof(T);
+template <typename T, int DK>
+struct Tile { __attribute__((aligned(16))) T q[kChunk][DK + kPad<T>], k[kChunk][DK + kPad<T>], v[kChunk][DK + kPad<T>]; };
+template <typename T, int DK>
 struct WalkLds {
-  __attribute__((aligned(16))) T k[kChunk][DK + 8];
-  __attribute__((aligned(16))) T v[kChunk][DV + 8];
-  __attribute__((aligned(16))) T state[NP][DV][DK + 8];      // transposed: columns of the state are rows here
-  __attribute__((aligned(16))) float weight[kChunk];
-  int bad;
+  Tile<T, DK> t[2];
+  __attribute__((aligned(16))) float weight[2][kChunk];             // of whole chunks, and of the last
+  int bad[2];
+  f32x4 earlier[DK <= 64 ? DK / 32 : 1][4][64];                     // two roles: as the accumulators hold it
 };
 
-// A block: one segment of one head and 32 or 64 columns of the state.  Waves share the chunk's queries (halves w & 1) and the columns
-// (halves w >> 1).
-template <typename T, int DK, int DV, bool VEC, bool FIN>
-__global__ void __launch_bounds__(4 * DV) k_linear_walk(LinearJobs jobs, LinearShape sh, int units, int cols, int njobs) {
-  constexpr int NT = 4 * DV, NP = sizeof(T) == 2 ? 2 : 1, NPS = sizeof(T) == 2 ? (FIN ? 3 : 2) : 1, NK = DK / 16, NTL = kTiles<DK>;
+// Waves for 32 columns: two of up to 64 wide heads (64 wide, 96 heads, 1024 positions, cut: forward 17.5 us with one, 14.5 with two),
+// one of wider ones (128 wide, 1024 sequences of 1024, forward: 307 us with one, 332 with two).
+template <int DK> constexpr int kRoles = DK <= 64 ? 2 : 1;
+template <typename T, int DK> constexpr int kWavesPerSimd = DK <= 64 ? (sizeof(T) == 2 ? 4 : 3) : sizeof(T) * DK == 512 ? 1 : 2;
+
+// A block: one segment of one head.
+template <typename T, int DK, bool VEC, bool FIN>
+__global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k_linear_walk(LinearJobs jobs, LinearShape sh, int units) {
+  constexpr int ROLES = kRoles<DK>, NT = 2 * ROLES * DK, NP = sizeof(T) == 2 ? 2 : 1, NPS = sizeof(T) == 2 ? (FIN ? 3 : 2) : 1, ND = DK / 32;
+  constexpr int LD = DK + kPad<T>;
   typedef typename Frag<T>::V FV;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  WalkLds<T, DK, DV, NP>& sm = *reinterpret_cast<WalkLds<T, DK, DV, NP>*>(smem);
+  WalkLds<T, DK>& sm = *reinterpret_cast<WalkLds<T, DK>*>(smem);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hf = lane >> 5;
-  const int qb = wave & 1, jb = wave >> 1;
-  // Blocks go to the eight dies by turns of their number: those that share a segment's rows are eight apart, on one die.
-  const int subs = cols * njobs, group = blockIdx.x / (8 * subs), rest = blockIdx.x % (8 * subs);
-  const int unit = group * 8 + rest % 8, sub = rest / 8;
-  if (unit >= units) return;
-  const LinearJob& job = jobs.j[sub / cols];
-  const int col0 = sub % cols * DV;
-  const int seg = unit % sh.segments, bh = unit / sh.segments, h = bh % sh.H, b = bh / sh.H, dh = sh.dh;
-  const int len = sh.length(b), first = seg * sh.per * kChunk;
-  const int last = first + sh.per * kChunk < sh.S ? first + sh.per * kChunk : sh.S;       // of the segment, padding included
-  const int stop = last < len ? last : len;
-  const float g2 = decay_of(sh.log_decay, h);
-  const int e0 = job.back ? 0 : 1;
-  const int hcols = dh - col0 < DV ? dh - col0 : DV;           // columns of the block that exist
-  // position u of the walk is row `at + u * dir`
-  const ptrdiff_t dir = job.back ? -1 : 1;
-  const size_t at = (size_t)b * sh.S + (job.back && len > 0 ? len - 1 : 0);
-  const T* qp = (const T*)job.q + (ptrdiff_t)at * job.ldq + h * dh;
-  const T* kp = (const T*)job.k + (ptrdiff_t)at * job.ldk + h * dh;
-  const T* vp = (const T*)job.v + (ptrdiff_t)at * job.ldv + h * dh + col0;
-  T* op = (T*)job.out + (ptrdiff_t)at * job.ldo + h * dh + col0;
+  const int col = wave < ND ? wave : wave - ND;
+  Place at;
+  if (!place(sh, units, at)) return;
+  const LinearJob job = jobs.j[at.job];
+  const int dh = sh.dh, e0 = job.back ? 0 : 1, first = at.first, stop = at.stop;
+  const bool back = job.back != 0, full = dh == DK;
+  // position u of the walk is row `row + u * dir`
+  const int dir = back ? -1 : 1;
+  const size_t row = at.row0 + (back && at.len > 0 ? at.len - 1 : 0);
+  const int head = kChunk < stop - first ? kChunk : stop - first;                // positions of the first chunk
+  const T* qp = lowest(column<T>(job.q, row, job.ldq, at.h, dh), job.ldq, back, first, head);
+  const T* kp = lowest(column<T>(job.k, row, job.ldk, at.h, dh), job.ldk, back, first, head);
+  const T* vp = lowest(column<T>(job.v, row, job.ldv, at.h, dh), job.ldv, back, first, head);
 
+  TileRegs<T, DK, kChunk, NT, VEC> qr, kr, vr;
+  int left = stop - first;                                   // positions not yet asked for
+  auto rows = [&](int count) {
+    qr.rows(job.ldq, back, count, dh);
+    kr.rows(job.ldk, back, count, dh);
+    vr.rows(job.ldv, back, count, dh);
+  };
+  auto fetch = [&]() {
+    const int count = left < kChunk ? left : kChunk;
+    if (count < kChunk) rows(count);
+    qr.load(qp, dh);
+    kr.load(kp, dh);
+    vr.load(vp, dh);
+    left -= count;
+    const int by = back ? -(left < kChunk ? left : kChunk) : kChunk;             // to the lowest row of the next chunk
+    qp += (ptrdiff_t)by * job.ldq;
+    kp += (ptrdiff_t)by * job.ldk;
+    vp += (ptrdiff_t)by * job.ldv;
+  };
+  auto leave = [&](int slot, int u0) {
+    qr.store(sm.t[slot].q, dh);
+    kr.store(sm.t[slot].k, dh);
+    if (vr.non_finite()) sm.bad[slot] = u0;
+    vr.store(sm.t[slot].v, dh);
+    if (left > 0) fetch();
+  };
+  if (first < stop) {
+    rows(head);
+    fetch();
+  }
   // rows of the padding are zeros, whatever stands there in the inputs
   {
-    T* pad = (T*)job.out + ((size_t)b * sh.S) * job.ldo + h * dh + col0;
-    const int from = first > len ? first : len;
-    for (int x = threadIdx.x; x < (last - from) * DV; x += NT)
-      if (x % DV < hcols) pad[(ptrdiff_t)(from + x / DV) * job.ldo + x % DV] = (T)0.f;
+    T* pad = const_cast<T*>(column<T>(job.out, at.row0, job.ldo, at.h, dh));
+    const int from = first > at.len ? first : at.len;
+    for (int x = threadIdx.x; x < (at.last - from) * DK; x += NT)
+      if (x % DK < dh) pad[(size_t)(from + x / DK) * job.ldo + x % DK] = (T)0.f;
   }
+  const int rest = (stop - first) % kChunk;
+  if (threadIdx.x < kChunk) {
+    const int u = threadIdx.x;
+    sm.weight[0][u] = power(at.g2, kChunk - u - e0);
+    sm.weight[1][u] = u < rest ? power(at.g2, rest - u - e0) : 0.f;
+  }
+  if (threadIdx.x < 2) sm.bad[threadIdx.x] = -1;
 
-  f32x16 state[NTL];
-  auto state_row = [&](int i, int v) { return 32 * qb + 64 * i + 8 * (v / 4) + 4 * hf + v % 4; };
-  const int scol = col0 + 32 * jb + n;
-  const bool owner = 32 * qb < DK;                             // heads of 32: the first of two waves holds the one tile
-  {
+  // The parts of the work on a chunk.
+  f32x16 state[ND];
+  const int scol = 32 * col + n;
+  auto pull = [&]() {                                        // the wave's columns of the state before the segment
     const bool whole = job.before != nullptr;
-    const float* x0 = whole ? job.before + ((size_t)bh * sh.segments + seg) * dh * dh : job.init ? job.init + (size_t)bh * dh * dh : nullptr;
-    const float f = whole ? 1.f : job.in_scale;
+    const float* x0 = whole ? job.before + ((size_t)at.bh * sh.segments + at.seg) * dh * dh : job.init ? job.init + (size_t)at.bh * dh * dh : nullptr;
 #pragma unroll
-    for (int i = 0; i < NTL; ++i)
+    for (int i = 0; i < ND; ++i) zero(state[i]);
+    if (!x0) return;
+    if (full) {
+      const float* x = job.turned ? x0 + scol * DK + 4 * hf : x0 + scol + 4 * hf * DK;
+      if (job.turned) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int r = state_row(i, v);
-        state[i][v] = 0.f;
-        if (x0 && r < dh && scol < dh) state[i][v] = f * (job.turned ? x0[(size_t)scol * dh + r] : x0[(size_t)r * dh + scol]);
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) state[i][v] = x[32 * i + acc_row(v, 0)];
+      } else {
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) state[i][v] = x[(32 * i + acc_row(v, 0)) * DK];
       }
-  }
-  auto publish = [&]() {                                       // the state as an operand, for all waves
-    if (!owner) return;
+    } else {
+      const int cc = scol < dh ? scol : dh - 1, by_row = job.turned ? 1 : dh, by_col = job.turned ? dh : 1;
+      const float* x = x0 + cc * by_col;
 #pragma unroll
-    for (int i = 0; i < NTL; ++i)
+      for (int i = 0; i < ND; ++i)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        typedef __attribute__((ext_vector_type(4))) T T4;
-        T4 part[NP];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float r = state[i][4 * g + j];
-#pragma unroll
-          for (int s = 0; s < NP; ++s) { part[s][j] = (T)r; r -= (float)part[s][j]; }
+        for (int v = 0; v < 16; ++v) {
+          const int r = 32 * i + acc_row(v, hf);
+          state[i][v] = x[(r < dh ? r : dh - 1) * by_row];
         }
 #pragma unroll
-        for (int s = 0; s < NP; ++s) *reinterpret_cast<T4*>(&sm.state[s][32 * jb + n][state_row(i, 4 * g)]) = part[s];
-      }
-  };
-
-  // decay between a query and the keys of its own 32 positions (nothing above the diagonal) and of the 32 before
-  float near[16], far[16];
+      for (int i = 0; i < ND; ++i)
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int r = 8 * (v / 4) + 4 * hf + v % 4;
-    near[v] = r <= n ? power(g2, n - r) * sh.scale : 0.f;
-    far[v] = power(g2, 32 + n - r) * sh.scale;
-  }
-  const float carry = power(g2, 32 * qb + n + e0) * sh.scale;
-
-  TileRegs<T, DK, NT, VEC> kr;
-  TileRegs<T, DV, NT, VEC> vr;
-  FV qf[NK], qn[NK];
-  auto fetch = [&](int u0) {
-    const int rows = stop - u0;
-    kr.load(kp + (ptrdiff_t)u0 * dir * job.ldk, dir * job.ldk, rows, dh);
-    vr.load(vp + (ptrdiff_t)u0 * dir * job.ldv, dir * job.ldv, rows, hcols);
-    const int u = 32 * qb + n;
-    const T* q = qp + (ptrdiff_t)(u0 + u) * dir * job.ldq;
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      const int c = 16 * kk + 8 * hf;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) qn[kk][e] = (T)0.f;
-      if (u < rows) {
-        if (VEC) {
-          if (c < dh) qn[kk] = frag_row(q + c);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (c + e < dh) qn[kk][e] = q[c + e];
-        }
-      }
+        for (int v = 0; v < 16; ++v) state[i][v] = 32 * i + acc_row(v, hf) < dh && scol < dh ? state[i][v] : 0.f;
     }
+    if (!whole && job.in_scale != 1.f) scale(state, job.in_scale);
   };
-  if (first < stop) fetch(first);
-  if (threadIdx.x == 0) sm.bad = -1;
-  int counted = -1;
-  for (int u0 = first; u0 < stop; u0 += kChunk) {
-    const int c = stop - u0 < kChunk ? stop - u0 : kChunk;
-    __syncthreads();                                           // the chunk before has been read
-    kr.store(sm.k);
-    vr.store(sm.v);
-    if (vr.non_finite()) sm.bad = u0;
-    publish();
-    if (c != counted && threadIdx.x < kChunk) sm.weight[threadIdx.x] = (int)threadIdx.x < c ? power(g2, c - threadIdx.x - e0) : 0.f;
-    counted = c;
+  auto earlier = [&](const Tile<T, DK>& t, float carry) {    // what the chunks before give
+    f32x16 o = (f32x16)0.f;
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) qf[kk] = qn[kk];
-    __syncthreads();
-    if (u0 + kChunk < stop) fetch(u0 + kChunk);
-    const bool slow = sm.bad == u0;
-
-    // what the earlier chunks give
-    f32x16 o;
-    zero(o);
-#pragma unroll
-    for (int s = NP - 1; s >= 0; --s)
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) o = mma(frag_row(&sm.state[s][32 * jb + n][16 * kk + 8 * hf]), qf[kk], o);
+    for (int kk = 0; kk < 2 * ND; ++kk) {
+      FV f[NP];
+      split_half(state[kk / 2], kk % 2, f);
+      o = mma_parts(f, frag_row<T>(&t.q[n][16 * kk + 4 * hf]), o);
+    }
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[v] *= carry;
+    return o;
+  };
+  auto own = [&](const Tile<T, DK>& t, f32x16 o, const float (&near)[16], bool slow, int c) {      // what the chunk itself adds
     if (!slow) {
-      // and the chunk itself; the scores above the diagonal are left out by choice and not by a product with 0, so that an
-      // infinity or a NaN in a later key reaches nobody
+      // the scores above the diagonal are left out by choice and not by a product with 0, so that an infinity or a NaN in a later
+      // key reaches nobody
+      f32x16 p = (f32x16)0.f;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (i > qb) break;
-        f32x16 p;
-        zero(p);
+      for (int kk = 0; kk < 2 * ND; ++kk) p = mma(frag_row<T>(&t.k[n][16 * kk + 4 * hf]), frag_row<T>(&t.q[n][16 * kk + 4 * hf]), p);
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk) p = mma(frag_row(&sm.k[32 * i + n][16 * kk + 8 * hf]), qf[kk], p);
-        const bool diagonal = i == qb;
+      for (int v = 0; v < 16; ++v) p[v] = acc_row(v, hf) <= n ? p[v] * near[v] : 0.f;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          f32x8 w;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int v = 8 * kk + e, r = 8 * (v / 4) + 4 * hf + v % 4;
-            w[e] = diagonal ? (r <= n ? p[v] * near[v] : 0.f) : p[v] * far[v];
-          }
-          FV f[NP];
-          split(w, f);
-          const FV a = frag_col<DV + 8>(sm.v, 32 * i + 16 * kk, 32 * jb, lane);
-#pragma unroll
-          for (int s = NP - 1; s >= 0; --s) o = mma(a, f[s], o);
-        }
+      for (int kk = 0; kk < 2; ++kk) {
+        FV f[NP];
+        split_half(p, kk, f);
+        o = mma_parts(frag_col<LD>(t.v, 16 * kk, 32 * col, lane), f, o);
       }
     } else {
       // A chunk with an infinity or a NaN among its values: row by row, the later ones left out (0 times infinity is not 0).
@@ -377,19 +436,27 @@ __global__ void __launch_bounds__(4 * DV) k_linear_walk(LinearJobs jobs, LinearS
       for (int r = 0; r < c; ++r) {
         float s = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk)
+        for (int kk = 0; kk < 2 * ND; ++kk) {
+          const FV k = frag_row<T>(&t.k[r][16 * kk + 4 * hf]), q = frag_row<T>(&t.q[n][16 * kk + 4 * hf]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) s = __builtin_fmaf((float)qf[kk][e], (float)sm.k[r][16 * kk + 8 * hf + e], s);
+          for (int e = 0; e < 8; ++e) s = __builtin_fmaf((float)q[e], (float)k[e], s);
+        }
         s += __shfl_xor(s, 32, 64);
-        const int away = 32 * qb + n - r;
-        if (away < 0) continue;
-        s *= power(g2, away) * sh.scale;
+        if (r > n) continue;
+        s *= power(at.g2, n - r) * sh.scale;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) o[v] = __builtin_fmaf(s, (float)sm.v[r][32 * jb + 8 * (v / 4) + 4 * hf + v % 4], o[v]);
+        for (int v = 0; v < 16; ++v) o[v] = __builtin_fmaf(s, (float)t.v[r][32 * col + acc_row(v, hf)], o[v]);
       }
     }
-    if (u0 + 32 * qb + n < stop) {
-      T* p = op + (ptrdiff_t)(u0 + 32 * qb + n) * dir * job.ldo + 32 * jb;
+    return o;
+  };
+  auto decays = [&](float (&near)[16]) {                     // between a query and the keys, dh^-1/2
+#pragma unroll
+    for (int v = 0; v < 16; ++v) near[v] = acc_row(v, hf) <= n ? power(at.g2, n - acc_row(v, hf)) * sh.scale : 0.f;
+  };
+  T* to = const_cast<T*>(column<T>(job.out, row, job.ldo, at.h, dh)) + ((ptrdiff_t)(first + n) * dir * job.ldo + 32 * col);
+  auto put = [&](const f32x16& o, int c) {
+    if (n < c) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         typedef __attribute__((ext_vector_type(4))) T T4;
@@ -398,40 +465,97 @@ __global__ void __launch_bounds__(4 * DV) k_linear_walk(LinearJobs jobs, LinearS
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = (T)o[4 * g + j];
         if (VEC) {
-          if (32 * jb + x < hcols) *reinterpret_cast<T4*>(p + x) = w;
+          if (full || 32 * col + x < dh) *reinterpret_cast<T4*>(to + x) = w;
         } else {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (32 * jb + x + j < hcols) p[x + j] = w[j];
+            if (32 * col + x + j < dh) to[x + j] = w[j];
         }
       }
     }
-    if (owner && (FIN || u0 + kChunk < stop)) {
-      const float keep = power(g2, c);
+    to += (ptrdiff_t)kChunk * dir * job.ldo;
+  };
+  const float carry = power(at.g2, n + e0) * sh.scale, keep_whole = power(at.g2, kChunk);
+  auto add = [&](const Tile<T, DK>& t, int c) {              // the chunk to the state
+    scale(state, c == kChunk ? keep_whole : power(at.g2, c));
+    add_outer<T, DK, NPS, LD>(state, t.k, t.v, sm.weight[c < kChunk], col, lane);
+  };
+  auto finish = [&]() {
+    if (!FIN || !job.fin) return;
+    float* out = job.fin + (size_t)at.bh * dh * dh;
 #pragma unroll
-      for (int i = 0; i < NTL; ++i)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) state[i][v] *= keep;
-      add_outer<T, DK, NPS, DK + 8, DV + 8>(state, sm.k, sm.v, sm.weight, qb, jb, lane);
-    }
-  }
-  if (FIN && job.fin && owner) {
-    float* out = job.fin + (size_t)bh * dh * dh;
-#pragma unroll
-    for (int i = 0; i < NTL; ++i)
+    for (int i = 0; i < ND; ++i)
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        const int r = state_row(i, v);
-        if (r < dh && scol < dh) out[(size_t)r * dh + scol] = state[i][v] * job.out_scale;
+        const int r = 32 * i + acc_row(v, hf);
+        if (full || (r < dh && scol < dh)) out[r * dh + scol] = state[i][v] * job.out_scale;
       }
+  };
+
+  // All waves go through the same chunks with as many barriers: behind the first the chunk's tile is there, behind the second (two
+  // roles) what the earlier chunks give.  The other tile is written behind the first barrier, when nobody reads it any more.
+  if constexpr (ROLES == 1) {
+    pull();
+    float near[16];
+    decays(near);
+    __syncthreads();
+    if (first < stop) leave(0, first);
+    for (int u0 = first, slot = 0; u0 < stop; u0 += kChunk, slot ^= 1) {
+      const int c = stop - u0 < kChunk ? stop - u0 : kChunk;
+      __syncthreads();
+      const Tile<T, DK>& t = sm.t[slot];
+      put(own(t, earlier(t, carry), near, sm.bad[slot] == u0, c), c);
+      if (FIN || u0 + kChunk < stop) add(t, c);
+      if (u0 + kChunk < stop) leave(slot ^ 1, u0 + kChunk);
+    }
+    finish();
+  } else if (wave < ND) {
+    pull();
+    __syncthreads();
+    if (first < stop) leave(0, first);
+    for (int u0 = first, slot = 0; u0 < stop; u0 += kChunk, slot ^= 1) {
+      const int c = stop - u0 < kChunk ? stop - u0 : kChunk;
+      __syncthreads();
+      const f32x16 o = earlier(sm.t[slot], carry);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = o[4 * g + j];
+        sm.earlier[col][g][lane] = w;
+      }
+      __syncthreads();
+      if (FIN || u0 + kChunk < stop) add(sm.t[slot], c);
+      if (u0 + kChunk < stop) leave(slot ^ 1, u0 + kChunk);
+    }
+    finish();
+  } else {
+    float near[16];
+    decays(near);
+    __syncthreads();
+    if (first < stop) leave(0, first);
+    for (int u0 = first, slot = 0; u0 < stop; u0 += kChunk, slot ^= 1) {
+      const int c = stop - u0 < kChunk ? stop - u0 : kChunk;
+      __syncthreads();
+      f32x16 o = own(sm.t[slot], (f32x16)0.f, near, sm.bad[slot] == u0, c);
+      __syncthreads();
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 w = sm.earlier[col][g][lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[4 * g + j] += w[j];
+      }
+      put(o, c);
+      if (u0 + kChunk < stop) leave(slot ^ 1, u0 + kChunk);
+    }
   }
 }
 
 // What a segment adds to the state: loc [B H, segments, dh, dh] for each job.  The last segment is needed only for the state that goes
-// out.  A block takes 64 columns.
+// out.
 struct StateJob {
   const void *k, *v;
-  int64_t ldk, ldv;
+  int ldk, ldv;
   float* loc;
   const float* init;
   float* fin;
@@ -440,95 +564,124 @@ struct StateJob {
 };
 struct StateJobs { StateJob j[2]; };
 
-template <typename T, int DK, int DV, bool VEC>
-__global__ void __launch_bounds__(4 * DV) k_linear_states(StateJobs jobs, LinearShape sh, int units, int cols, int njobs) {
-  constexpr int NT = 4 * DV, NPS = sizeof(T) == 2 ? 3 : 1, NTL = kTiles<DK>;
-  __shared__ __attribute__((aligned(16))) T ks[kChunk][DK + 8], vs[kChunk][DV + 8];
-  __shared__ __attribute__((aligned(16))) float weight[kChunk];
+// Two waves for every 32 columns, which take a half of every 64 positions each; their sums are added at the end.
+template <typename T, int DK, bool VEC, bool FIN>
+__global__ void __launch_bounds__(4 * DK) k_linear_states(StateJobs jobs, LinearShape sh, int units) {
+  constexpr int NPS = sizeof(T) == 2 ? (FIN ? 3 : 2) : 1, ND = DK / 32, LD = DK + kPad<T>, R = 2 * kChunk;
+  struct Lds { __attribute__((aligned(16))) T k[2][R][LD], v[2][R][LD]; __attribute__((aligned(16))) float weight[2][R]; };
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  Lds& sm = *reinterpret_cast<Lds*>(smem);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hf = lane >> 5;
-  const int ib = wave & 1, jb = wave >> 1;
-  const int subs = cols * njobs, group = blockIdx.x / (8 * subs), rest = blockIdx.x % (8 * subs);
-  const int unit = group * 8 + rest % 8, sub = rest / 8;
-  if (unit >= units) return;
-  const StateJob& job = jobs.j[sub / cols];
-  const int col0 = sub % cols * DV;
-  const int seg = unit % sh.segments, bh = unit / sh.segments, h = bh % sh.H, b = bh / sh.H, dh = sh.dh;
-  if (seg == sh.segments - 1 && !job.fin) return;
-  const int len = sh.length(b), first = seg * sh.per * kChunk;
-  const int stop = first + sh.per * kChunk < len ? first + sh.per * kChunk : len;
-  const float g2 = decay_of(sh.log_decay, h);
-  const int e0 = job.back ? 0 : 1;
-  const int hcols = dh - col0 < DV ? dh - col0 : DV;
-  const ptrdiff_t dir = job.back ? -1 : 1;
-  const size_t at = (size_t)b * sh.S + (job.back && len > 0 ? len - 1 : 0);
-  const T* kp = (const T*)job.k + (ptrdiff_t)at * job.ldk + h * dh;
-  const T* vp = (const T*)job.v + (ptrdiff_t)at * job.ldv + h * dh + col0;
-  const bool owner = 32 * ib < DK;
-  f32x16 state[NTL];
+  const int half = wave / ND, col = wave % ND;
+  Place at;
+  if (!place(sh, units, at)) return;
+  const StateJob job = jobs.j[at.job];
+  if (at.seg == sh.segments - 1 && !job.fin) return;
+  const int dh = sh.dh, e0 = job.back ? 0 : 1, first = at.first, stop = at.stop;
+  const bool back = job.back != 0, full = dh == DK;
+  const size_t row = at.row0 + (back && at.len > 0 ? at.len - 1 : 0);
+  const int head = R < stop - first ? R : stop - first;
+  const T* kp = lowest(column<T>(job.k, row, job.ldk, at.h, dh), job.ldk, back, first, head);
+  const T* vp = lowest(column<T>(job.v, row, job.ldv, at.h, dh), job.ldv, back, first, head);
+  f32x16 state[ND];
 #pragma unroll
-  for (int i = 0; i < NTL; ++i) zero(state[i]);
-  TileRegs<T, DK, NT, VEC> kr;
-  TileRegs<T, DV, NT, VEC> vr;
-  auto fetch = [&](int u0) {
-    kr.load(kp + (ptrdiff_t)u0 * dir * job.ldk, dir * job.ldk, stop - u0, dh);
-    vr.load(vp + (ptrdiff_t)u0 * dir * job.ldv, dir * job.ldv, stop - u0, hcols);
-  };
-  if (first < stop) fetch(first);
-  for (int u0 = first; u0 < stop; u0 += kChunk) {
-    const int c = stop - u0 < kChunk ? stop - u0 : kChunk;
-    __syncthreads();
-    kr.store(ks);
-    vr.store(vs);
-    if (threadIdx.x < kChunk) weight[threadIdx.x] = (int)threadIdx.x < c ? power(g2, c - threadIdx.x - e0) : 0.f;
-    __syncthreads();
-    if (u0 + kChunk < stop) fetch(u0 + kChunk);
-    if (owner) {
-      const float keep = power(g2, c);
-#pragma unroll
-      for (int i = 0; i < NTL; ++i)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) state[i][v] *= keep;
-      add_outer<T, DK, NPS, DK + 8, DV + 8>(state, ks, vs, weight, ib, jb, lane);
+  for (int i = 0; i < ND; ++i) zero(state[i]);
+  TileRegs<T, DK, R, 4 * DK, VEC> kr, vr;
+  int left = stop - first;
+  auto fetch = [&]() {
+    const int count = left < R ? left : R;
+    if (count < R) {
+      kr.rows(job.ldk, back, count, dh);
+      vr.rows(job.ldv, back, count, dh);
     }
+    kr.load(kp, dh);
+    vr.load(vp, dh);
+    left -= count;
+    const int by = back ? -(left < R ? left : R) : R;
+    kp += (ptrdiff_t)by * job.ldk;
+    vp += (ptrdiff_t)by * job.ldv;
+  };
+  if (first < stop) {
+    kr.rows(job.ldk, back, head, dh);
+    vr.rows(job.ldv, back, head, dh);
+    fetch();
   }
-  if (!owner) return;
-  float* out = job.loc + ((size_t)bh * sh.segments + seg) * dh * dh;
-  const int scol = col0 + 32 * jb + n;
+  const int rest = (stop - first) % R;
+  if (threadIdx.x < R) {
+    const int u = threadIdx.x;
+    sm.weight[0][u] = power(at.g2, R - u - e0);
+    sm.weight[1][u] = u < rest ? power(at.g2, rest - u - e0) : 0.f;
+  }
+  const float keep_whole = power(at.g2, R);
+  for (int u0 = first, slot = 0; u0 < stop; u0 += R, slot ^= 1) {
+    const int c = stop - u0 < R ? stop - u0 : R;
+    kr.store(sm.k[slot], dh);                                // read by nobody since the last barrier
+    vr.store(sm.v[slot], dh);
+    if (left > 0) fetch();
+    __syncthreads();
+    scale(state, c == R ? keep_whole : power(at.g2, c));
+    add_outer<T, DK, NPS, LD>(state, sm.k[slot] + kChunk * half, sm.v[slot] + kChunk * half, sm.weight[c < R] + kChunk * half, col, lane);
+  }
+  // the second halves' sums go through the tiles' memory
+  float* part = reinterpret_cast<float*>(smem) + col * (ND * 16 * 64);
+  __syncthreads();
+  if (half == 1) {
 #pragma unroll
-  for (int i = 0; i < NTL; ++i)
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) part[(i * 16 + v) * 64 + lane] = state[i][v];
+  }
+  __syncthreads();
+  if (half == 1) return;
+  float* out = job.loc + ((size_t)at.bh * sh.segments + at.seg) * dh * dh;
+  const int scol = 32 * col + n;
+#pragma unroll
+  for (int i = 0; i < ND; ++i)
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      const int r = 32 * ib + 64 * i + 8 * (v / 4) + 4 * hf + v % 4;
-      if (r < dh && scol < dh) out[(size_t)r * dh + scol] = state[i][v];
+      const int r = 32 * i + acc_row(v, hf);
+      if (full || (r < dh && scol < dh)) out[r * dh + scol] = state[i][v] + part[(i * 16 + v) * 64 + lane];
     }
 }
+template <typename T, int DK>
+constexpr int state_lds() {
+  const int tiles = 2 * 2 * 2 * kChunk * (DK + kPad<T>) * (int)sizeof(T) + 2 * 2 * kChunk * 4, sums = DK / 32 * (DK / 32) * 16 * 64 * 4;
+  return tiles > sums ? tiles : sums;
+}
 
-// In place: what a segment adds becomes the state before it.  One thread an element of the state.
+// In place: what a segment adds becomes the state before it.  A thread takes V neighbouring elements of the state.
+template <int V>
 __global__ void __launch_bounds__(256) k_linear_scan(StateJobs jobs, LinearShape sh) {
-  const StateJob& job = jobs.j[blockIdx.z];
-  const int bh = blockIdx.y, x = blockIdx.x * 256 + threadIdx.x, dd = sh.dh * sh.dh;
+  typedef __attribute__((ext_vector_type(V))) float FV;
+  const StateJob job = jobs.j[blockIdx.z];
+  const int bh = blockIdx.y, x = (blockIdx.x * 256 + threadIdx.x) * V, dd = sh.dh * sh.dh;
   if (x >= dd) return;
+  float* p = job.loc + (size_t)bh * sh.segments * dd + x;
+  const int last = job.fin ? sh.segments : sh.segments - 1;    // segments whose addition is there
+  constexpr int U = 8;                                         // loads in flight
+  FV add[U], s = (FV)0.f;
+  auto fetch = [&](int g) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) add[i] = g + i < last ? *reinterpret_cast<const FV*>(p + (size_t)(g + i) * dd) : (FV)0.f;
+  };
+  fetch(0);
+  if (job.init) s = *reinterpret_cast<const FV*>(job.init + (size_t)bh * dd + x) * job.in_scale;
   const float g2 = decay_of(sh.log_decay, bh % sh.H);
   const int len = sh.length(bh / sh.H), span = sh.per * kChunk;
-  float s = job.init ? job.init[(size_t)bh * dd + x] * job.in_scale : 0.f;
-  float* p = job.loc + (size_t)bh * sh.segments * dd + x;
-  constexpr int U = 8;                         // loads in flight
   for (int g = 0; g < sh.segments; g += U) {
-    float add[U];
+    FV now[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const bool there = g + i < sh.segments - 1 || (g + i == sh.segments - 1 && job.fin);
-      add[i] = there ? p[(size_t)(g + i) * dd] : 0.f;
-    }
+    for (int i = 0; i < U; ++i) now[i] = add[i];
+    if (g + U < sh.segments) fetch(g + U);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       if (g + i >= sh.segments) break;
-      p[(size_t)(g + i) * dd] = s;
+      *reinterpret_cast<FV*>(p + (size_t)(g + i) * dd) = s;
       const int left = len - (g + i) * span, c = left < 0 ? 0 : left < span ? left : span;
-      s = power(g2, c) * s + add[i];
+      s = power(g2, c) * s + now[i];
     }
   }
-  if (job.fin) job.fin[(size_t)bh * dd + x] = s * job.out_scale;
+  if (job.fin) *reinterpret_cast<FV*>(job.fin + (size_t)bh * dd + x) = s * job.out_scale;
 }
 
 // One position: the state is read, decayed, added to and written back; a wave takes `rows` of its rows at a time.
@@ -590,45 +743,49 @@ __global__ void __launch_bounds__(256) k_linear_step(const T* __restrict__ qkv, 
 
 constexpr int kMaxHead = 128;
 
-// Segments of a sequence: enough blocks for the chip, none of less than two chunks.
+// Segments of a sequence: as many as give 768 blocks, three or so for each compute unit, but none of less than four chunks, and
+// no cut into two, which costs two more launches and a second pass over k and v.  (Forward and backward, us: 96 heads of 64, 1024 positions,
+// for 384 / 768 / 1536 blocks 33 + 53, 32 + 54, 32 + 59; 16 heads, 16384 positions 61 + 135, 56 + 103, 66 + 112.  Of two chunks:
+// 32 heads in fp32, 2048 positions 62 + 95 instead of 47 + 95.  In two: 8 heads, 300 positions 18 + 19, uncut 15 + 15.)
 struct Cut { int segments, per; };
-Cut cut_of(int B, int S, int H, int dh, int jobs) {
+Cut cut_of(int B, int S, int H, int jobs) {
   const int chunks = (S + kChunk - 1) / kChunk;
-  const long blocks = (long)B * H * jobs * (dh > 64 ? 2 : 1);
-  long want = blocks > 0 ? (1024 + blocks - 1) / blocks : 1;
-  const long most = chunks / 2 > 0 ? chunks / 2 : 1;
+  const long blocks = (long)B * H * jobs;
+  long want = blocks > 0 ? 768 / blocks : 1;
+  const long most = chunks / 4;
   if (want > most) want = most;
+  if (want < 3) want = 1;
   Cut c;
   c.per = chunks > 0 ? (int)((chunks + want - 1) / want) : 1;
   c.segments = chunks > 0 ? (chunks + c.per - 1) / c.per : 1;
   return c;
 }
 
-// Launches a kernel for a head size; F is called with (integral DK, DV, bool VEC).
+// Calls fn(integral DK, bool VEC) for a head size.
 template <typename F>
 hipError_t by_head(int dh, bool vec, F&& fn) {
   auto go = [&](auto v) {
-    if (dh <= 32) return fn(std::integral_constant<int, 32>(), std::integral_constant<int, 32>(), v);
-    if (dh <= 64) return fn(std::integral_constant<int, 64>(), std::integral_constant<int, 64>(), v);
-    return fn(std::integral_constant<int, 128>(), std::integral_constant<int, 64>(), v);
+    if (dh <= 32) return fn(std::integral_constant<int, 32>(), v);
+    if (dh <= 64) return fn(std::integral_constant<int, 64>(), v);
+    if (dh <= 96) return fn(std::integral_constant<int, 96>(), v);
+    return fn(std::integral_constant<int, 128>(), v);
   };
   return vec ? go(std::true_type()) : go(std::false_type());
 }
 
 template <typename T>
 hipError_t walk(const OpCtx& c, const LinearJobs& jobs, int njobs, const LinearShape& sh, bool vec, bool fin) {
-  const int cols = sh.dh > 64 ? 2 : 1, units = sh.B * sh.H * sh.segments;
-  return by_head(sh.dh, vec, [&](auto dk, auto dv, auto v) {
-    constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
+  const int units = sh.B * sh.H * sh.segments;
+  const dim3 blocks(8, njobs, (units + 7) / 8);
+  return by_head(sh.dh, vec, [&](auto dk, auto v) {
+    constexpr int DK = decltype(dk)::value, lds = (int)sizeof(WalkLds<T, DK>), threads = 2 * kRoles<DK> * DK;
     constexpr bool VEC = decltype(v)::value;
-    constexpr int lds = (int)sizeof(WalkLds<T, DK, DV, sizeof(T) == 2 ? 2 : 1>);
-    const int blocks = (units + 7) / 8 * 8 * cols * njobs;
     auto go = [&](auto f) {
       constexpr bool FIN = decltype(f)::value;
       static LdsLimit limit;
-      const hipError_t e = limit.raise(reinterpret_cast<const void*>(k_linear_walk<T, DK, DV, VEC, FIN>), lds);
+      const hipError_t e = limit.raise(reinterpret_cast<const void*>(k_linear_walk<T, DK, VEC, FIN>), lds);
       if (e != hipSuccess) return e;
-      k_linear_walk<T, DK, DV, VEC, FIN><<<blocks, 4 * DV, lds, c.stream>>>(jobs, sh, units, cols, njobs);
+      k_linear_walk<T, DK, VEC, FIN><<<blocks, threads, lds, c.stream>>>(jobs, sh, units);
       return hipGetLastError();
     };
     return fin ? go(std::true_type()) : go(std::false_type());
@@ -636,20 +793,34 @@ hipError_t walk(const OpCtx& c, const LinearJobs& jobs, int njobs, const LinearS
 }
 template <typename T>
 hipError_t states(const OpCtx& c, const StateJobs& jobs, int njobs, const LinearShape& sh, bool vec) {
-  const int cols = sh.dh > 64 ? 2 : 1, units = sh.B * sh.H * sh.segments;
-  const hipError_t e = by_head(sh.dh, vec, [&](auto dk, auto dv, auto v) {
-    constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
-    k_linear_states<T, DK, DV, decltype(v)::value><<<(units + 7) / 8 * 8 * cols * njobs, 4 * DV, 0, c.stream>>>(jobs, sh, units, cols, njobs);
-    return hipGetLastError();
+  const int units = sh.B * sh.H * sh.segments;
+  const dim3 blocks(8, njobs, (units + 7) / 8);
+  const hipError_t e = by_head(sh.dh, vec, [&](auto dk, auto v) {
+    constexpr int DK = decltype(dk)::value, lds = state_lds<T, DK>();
+    constexpr bool VEC = decltype(v)::value;
+    auto go = [&](auto f) {
+      constexpr bool FIN = decltype(f)::value;
+      static LdsLimit limit;
+      const hipError_t le = limit.raise(reinterpret_cast<const void*>(k_linear_states<T, DK, VEC, FIN>), lds);
+      if (le != hipSuccess) return le;
+      k_linear_states<T, DK, VEC, FIN><<<blocks, 4 * DK, lds, c.stream>>>(jobs, sh, units);
+      return hipGetLastError();
+    };
+    return jobs.j[0].fin || jobs.j[1].fin ? go(std::true_type()) : go(std::false_type());
   });
   if (e != hipSuccess) return e;
-  k_linear_scan<<<dim3((sh.dh * sh.dh + 255) / 256, sh.B * sh.H, njobs), 256, 0, c.stream>>>(jobs, sh);
+  uintptr_t low = 0;
+  for (int i = 0; i < njobs; ++i) low |= (uintptr_t)jobs.j[i].loc | (uintptr_t)jobs.j[i].init | (uintptr_t)jobs.j[i].fin;
+  const int dd = sh.dh * sh.dh;
+  if (dd % 4 == 0 && (low & 15) == 0) k_linear_scan<4><<<dim3((dd / 4 + 255) / 256, sh.B * sh.H, njobs), 256, 0, c.stream>>>(jobs, sh);
+  else k_linear_scan<1><<<dim3((dd + 255) / 256, sh.B * sh.H, njobs), 256, 0, c.stream>>>(jobs, sh);
   return hipGetLastError();
 }
 
 bool shape_ok(int dt, int B, int S, int H, int dh) {
   return (dt == F32 || dt == BF16) && B >= 0 && S >= 0 && H >= 1 && dh >= 1 && dh <= kMaxHead && (int64_t)B * H <= 65535 &&
-         (int64_t)3 * H * dh <= 0x7fffffff && S <= 0x7fffffff - 2 * kChunk;
+         (int64_t)3 * H * dh < 1 << 24 &&       // offsets inside a chunk: 24-bit rows, 32-bit bytes
+         S <= 0x7fffffff - 4 * kChunk && (int64_t)B * H * (S / kChunk + 1) <= 0x7fffffff / 32;
 }
 LinearShape shape_of(const Cut& cut, const float* log_decay, const int32_t* lens, int B, int S, int H, int dh) {
   LinearShape sh;
@@ -669,7 +840,7 @@ bool whole_chunks(int dh, std::initializer_list<const void*> bufs) {
 
 size_t linear_attn_scratch(int B, int S, int H, int dh, bool backward) {
   if (!shape_ok(BF16, B, S, H, dh)) return 0;
-  const Cut cut = cut_of(B, S, H, dh, backward ? 3 : 1);
+  const Cut cut = cut_of(B, S, H, backward ? 3 : 1);
   return cut.segments > 1 ? (size_t)B * H * cut.segments * dh * dh * (backward ? 2 : 1) : 0;
 }
 
@@ -679,11 +850,12 @@ hipError_t op_linear_attn_fwd(const OpCtx& c, const void* qkv, const float* log_
   if (!shape_ok(c.dt, B, S, H, dh)) return hipErrorInvalidValue;
   if (B == 0) return hipSuccess;
   if (!log_decay || (S > 0 && (!qkv || !o))) return hipErrorInvalidValue;
-  const Cut cut = cut_of(B, S, H, dh, 1);
+  const Cut cut = cut_of(B, S, H, 1);
   if (cut.segments > 1 && (!c.partial || c.partial_elems < linear_attn_scratch(B, S, H, dh, false))) return hipErrorInvalidValue;
   const LinearShape sh = shape_of(cut, log_decay, lens, B, S, H, dh);
   const bool vec = whole_chunks(dh, {qkv, o});
-  const size_t e = dtype_size(c.dt), d = (size_t)H * dh;
+  const size_t e = dtype_size(c.dt);
+  const int d = H * dh;
   const char* p = (const char*)qkv;
   LinearJobs jobs = {};
   LinearJob& j = jobs.j[0];
@@ -708,22 +880,23 @@ hipError_t op_linear_attn_bwd(const OpCtx& c, const void* qkv, const float* log_
   if (!shape_ok(c.dt, B, S, H, dh)) return hipErrorInvalidValue;
   if (B == 0) return hipSuccess;
   if (!log_decay || (S > 0 && (!qkv || !dout || !dqkv))) return hipErrorInvalidValue;
-  const Cut cut = cut_of(B, S, H, dh, 3);
+  const Cut cut = cut_of(B, S, H, 3);
   if (cut.segments > 1 && (!c.partial || c.partial_elems < linear_attn_scratch(B, S, H, dh, true))) return hipErrorInvalidValue;
   const LinearShape sh = shape_of(cut, log_decay, lens, B, S, H, dh);
   const bool vec = whole_chunks(dh, {qkv, dout, dqkv});
-  const size_t e = dtype_size(c.dt), d = (size_t)H * dh;
+  const size_t e = dtype_size(c.dt);
+  const int d = H * dh;
   const char *q = (const char*)qkv, *k = q + d * e, *v = k + d * e;
   char* dq = (char*)dqkv;
   const float up = (float)sqrt((double)dh);        // the states of the way back are kept without the factor dh^-1/2
-  auto job = [&](const void* jq, int64_t ldq, const void* jk, int64_t ldk, const void* jv, int64_t ldv, void* out, int back) {
+  auto job = [&](const void* jq, int ldq, const void* jk, int ldk, const void* jv, int ldv, void* out, int back) {
     LinearJob j = {};
     j.q = jq; j.ldq = ldq; j.k = jk; j.ldk = ldk; j.v = jv; j.ldv = ldv; j.out = out; j.ldo = 3 * d; j.back = back;
     j.in_scale = back ? up : 1.f; j.out_scale = sh.scale;
     j.init = back ? ds_out : s0;
     return j;
   };
-  const int64_t w = 3 * d;
+  const int w = 3 * d;
   LinearJobs jobs;
   jobs.j[0] = job(dout, d, v, w, k, w, dq, 0);                      // dQ
   jobs.j[1] = job(k, w, q, w, dout, d, dq + 2 * d * e, 1);          // dV
