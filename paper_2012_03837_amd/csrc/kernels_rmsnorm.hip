@@ -11,8 +11,6 @@
 
 namespace lp {
 
-hipError_t op_reduce_partials(const OpCtx& c, const float* partial, int nblk, int n, float* out, int accumulate);
-
 namespace {
 
 // ------------------------------------------------------------------------------------------------ dropout
@@ -62,20 +60,53 @@ __device__ __forceinline__ float row_all(float v, float* sh) {
   }
   return v;
 }
-template <int V, typename T>
-__device__ __forceinline__ void load_v(const T* p, float (&v)[V]) {
-  if constexpr (V == 8) load8(p, v);
-  else v[0] = to_f(*p);
-}
+// V elements as they stand in memory: loads that are asked for long before they are used.
+template <typename T, int V> struct Raw;
+template <> struct Raw<bf16_t, 8> {
+  bf16x8 a;
+  __device__ __forceinline__ void load(const bf16_t* p) { a = *reinterpret_cast<const bf16x8*>(p); }
+  __device__ __forceinline__ void zero() { a = (bf16x8)(bf16_t)0.f; }
+  __device__ __forceinline__ float operator[](int e) const { return (float)a[e]; }
+  // what has been computed from it so far is not kept in registers (a conversion costs less than twice the registers)
+  __device__ __forceinline__ void again() {
+    typedef __attribute__((ext_vector_type(4))) unsigned U;
+    U w = __builtin_bit_cast(U, a);
+    asm volatile("" : "+v"(w));
+    a = __builtin_bit_cast(bf16x8, w);
+  }
+};
+template <> struct Raw<float, 8> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const f32x4*>(p); b = *reinterpret_cast<const f32x4*>(p + 4); }
+  __device__ __forceinline__ void zero() { a = (f32x4)0.f; b = (f32x4)0.f; }
+  __device__ __forceinline__ float operator[](int e) const { return e < 4 ? a[e] : b[e - 4]; }
+  __device__ __forceinline__ void again() { asm volatile("" : "+v"(a), "+v"(b)); }
+};
+template <typename T> struct Raw<T, 1> {
+  T a;
+  __device__ __forceinline__ void load(const T* p) { a = *p; }
+  __device__ __forceinline__ void zero() { a = (T)0.f; }
+  __device__ __forceinline__ float operator[](int) const { return to_f(a); }
+  __device__ __forceinline__ void again() {}
+};
 template <int V, typename T>
 __device__ __forceinline__ void store_v(T* p, const float (&v)[V]) {
   if constexpr (V == 8) store8(p, v);
   else *p = from_f<T>(v[0]);
 }
-template <int V>
-__device__ __forceinline__ void drop_v(const Drop& d, const PhiloxKey& key, size_t i, float (&v)[V]) {
-  if constexpr (V == 8) drop8(d, key, (unsigned)(i >> 3), v);
-  else v[0] = drop1(d, key, i, v[0]);
+// One element a lane: eight neighbours would draw the same four words.  The lanes of a row draw them once, a counter each, and
+// leave them in LDS, where element j's number stands at (first & 7) + j.  (37000 rows of 449, bf16: forward 58 us
+// with every lane's own words, 39 so; backward 60 and 37.)
+template <int LPR, int NCH> struct Numbers { uint4 w[LPR * NCH / 8 + 2]; };
+template <int LPR, int NCH>
+__device__ __forceinline__ void draw_row(const Drop& d, const PhiloxKey& key, size_t first, int width, Numbers<LPR, NCH>& num) {
+  const int groups = ((int)(first & 7) + width + 7) >> 3;
+  for (int k = threadIdx.x % LPR; k < groups; k += LPR) num.w[k] = philox(key, (unsigned)(first >> 3) + k, d.site);
+}
+template <int LPR, int NCH, int V>
+__device__ __forceinline__ void drop_v(const Drop& d, const PhiloxKey& key, size_t first, int j, const Numbers<LPR, NCH>& num, float (&v)[V]) {
+  if constexpr (V == 8) drop8(d, key, (unsigned)((first + j) >> 3), v);
+  else v[0] = reinterpret_cast<const unsigned short*>(num.w)[(first & 7) + j] >= d.thr ? v[0] * d.factor : 0.f;
 }
 __device__ __forceinline__ unsigned char to_e4m3(float a) {
   return (unsigned char)(__builtin_amdgcn_cvt_pk_fp8_f32(a, a, 0, false) & 0xff);
@@ -89,38 +120,43 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_fwd(const T* x, const T
                                                              float* __restrict__ rstd, int rows, int d, float eps, Drop dr) {
   __shared__ float sh[16];
   constexpr int RPB = threads_of(LPR) / LPR;
+  __shared__ Numbers<LPR, V == 1 ? NCH : 0> numbers[RPB];
+  auto& num = numbers[threadIdx.x / LPR];
   const int lane = threadIdx.x % LPR, row = blockIdx.x * RPB + threadIdx.x / LPR;
   const bool live = row < rows;                 // rows share a wave: those past the end go along in its shuffles
   const size_t base = (size_t)row * d;
-  const PhiloxKey key = philox_key(dr);
   const int d_live = live ? d : 0;
+  Raw<T, V> xr[NCH], rr[NCH];
+  Raw<float, V> gr[NCH];
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    const int j = (lane + LPR * i) * V;
+    xr[i].zero();
+    rr[i].zero();
+    gr[i].zero();
+    if (j < d_live) {
+      xr[i].load(x + base + j);
+      if (res) rr[i].load(res + base + j);
+      gr[i].load(g + j);
+    }
+  }
+  const PhiloxKey key = philox_key(dr);
+  if (V == 1 && dr.thr) {
+    draw_row(dr, key, base, d, num);
+    __syncthreads();
+  }
   float v[NCH][V], s = 0.f;
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
     const int j = (lane + LPR * i) * V;
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[i][e] = 0.f;
-    if (j < d_live) load_v<V>(x + base + j, v[i]);
-  }
-  if (dr.thr) {
+    for (int e = 0; e < V; ++e) v[i][e] = xr[i][e];
+    if (dr.thr && (V == 8 || j < d)) drop_v(dr, key, base, j, num, v[i]);
+    if (res) {
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int j = (lane + LPR * i) * V;
-      if (j < d_live) drop_v<V>(dr, key, base + j, v[i]);
+      for (int e = 0; e < V; ++e) v[i][e] += rr[i][e];
     }
-  }
-#pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    const int j = (lane + LPR * i) * V;
-    if (j < d_live) {
-      if (res) {
-        float t[V];
-        load_v<V>(res + base + j, t);
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[i][e] += t[e];
-      }
-      if (r) store_v<V>(r + base + j, v[i]);
-    }
+    if (r && j < d_live) store_v<V>(r + base + j, v[i]);
 #pragma unroll
     for (int e = 0; e < V; ++e) s += v[i][e] * v[i][e];
   }
@@ -132,11 +168,9 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_fwd(const T* x, const T
   for (int i = 0; i < NCH; ++i) {
     const int j = (lane + LPR * i) * V;
     if (j < d_live) {
-      float gg[V];
-      load_v<V>(g + j, gg);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        v[i][e] = v[i][e] * rs * gg[e];
+        v[i][e] = v[i][e] * rs * gr[i][e];
         const float a = fabsf(v[i][e]);
         top = a > top || a != a ? a : top;
       }
@@ -168,47 +202,77 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_fwd(const T* x, const T
   }
 }
 
-// Blocks walk over the rows with a stride and keep the sums of dg of their columns in registers; partial[block][d].
+// Blocks walk over the rows with a stride and keep the sums of dg of their columns in registers; partial[block][d].  A row stays in
+// registers as it was loaded, and where that is little enough the next one's loads are under way beside it.
 template <typename T, int LPR, int NCH, int V>
-__global__ void __launch_bounds__(threads_of(LPR)) k_rms_bwd(const T* dy, const T* r, const float* __restrict__ rstd,
+__global__ void __launch_bounds__(threads_of(LPR), 4) k_rms_bwd(const T* dy, const T* r, const float* __restrict__ rstd,
                                                              const float* __restrict__ g, const T* add, T* dres, T* dx,
                                                              float* __restrict__ partial, int rows, int d, Drop dr) {
-  constexpr int RPB = threads_of(LPR) / LPR;
+  constexpr int RPB = threads_of(LPR) / LPR, REGS = V == 8 ? NCH * 2 * (int)sizeof(T) : NCH;
+  constexpr bool AHEAD = REGS <= (V == 8 ? 4 : 8);
   __shared__ float sh[16];
+  __shared__ Numbers<LPR, V == 1 ? NCH : 0> numbers[RPB];
   extern __shared__ float sums[];               // [RPB][LPR * NCH * V], where a block has several rows
   const int lane = threadIdx.x % LPR, sub = threadIdx.x / LPR;
-  const PhiloxKey key = philox_key(dr);
-  float gg[NCH][V], pg[NCH][V];
-#pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    const int j = (lane + LPR * i) * V;
-#pragma unroll
-    for (int e = 0; e < V; ++e) { pg[i][e] = 0.f; gg[i][e] = 0.f; }
-    if (j < d) load_v<V>(g + j, gg[i]);
-  }
-  for (int row0 = blockIdx.x * RPB; row0 < rows; row0 += gridDim.x * RPB) {
-    const bool live = row0 + sub < rows;
-    const int row = live ? row0 + sub : rows - 1;
+  auto& num = numbers[sub];
+  struct Row { Raw<T, V> r[NCH], y[NCH], a[NCH]; float rs; } now, next;
+  auto fetch = [&](int row, Row& to) {
+    const bool live = row < rows;               // rows share a wave: those past the end go along in its shuffles
     const size_t base = (size_t)row * d;
-    const float rs = live ? rstd[row] : 0.f;
-    float xh[NCH][V], a[NCH][V], s = 0.f;
+    to.rs = live ? rstd[row] : 0.f;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int j = (lane + LPR * i) * V;
-#pragma unroll
-      for (int e = 0; e < V; ++e) { xh[i][e] = 0.f; a[i][e] = 0.f; }
-      if (j < d && live) { load_v<V>(r + base + j, xh[i]); load_v<V>(dy + base + j, a[i]); }
+      to.r[i].zero();
+      to.y[i].zero();
+      to.a[i].zero();
+      if (j < d && live) {
+        to.r[i].load(r + base + j);
+        to.y[i].load(dy + base + j);
+        if (add) to.a[i].load(add + base + j);
+      }
     }
+  };
+  if (AHEAD) fetch(blockIdx.x * RPB + sub, next);
+  const PhiloxKey key = philox_key(dr);
+  Raw<float, V> gg[NCH];
+  float pg[NCH][V];
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    const int j = (lane + LPR * i) * V;
+    gg[i].zero();
+    if (j < d) gg[i].load(g + j);
+#pragma unroll
+    for (int e = 0; e < V; ++e) pg[i][e] = 0.f;
+  }
+  for (int row0 = blockIdx.x * RPB; row0 < rows; row0 += gridDim.x * RPB) {
+    const int row = row0 + sub;
+    const bool live = row < rows;
+    const size_t base = (size_t)row * d;
+    if (AHEAD) {
+      now = next;
+      if (row0 + (int)gridDim.x * RPB < rows) fetch(row + gridDim.x * RPB, next);
+    } else {
+      fetch(row, now);
+    }
+    const float rs = now.rs;
+    float s = 0.f;
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        xh[i][e] *= rs;
-        pg[i][e] += a[i][e] * xh[i][e];
-        a[i][e] *= gg[i][e];
-        s += a[i][e] * xh[i][e];
+        const float yx = now.y[i][e] * (now.r[i][e] * rs);
+        pg[i][e] += yx;
+        s += yx * gg[i][e];
       }
     s = row_all<LPR, false>(s, sh) / (float)d;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) { now.r[i].again(); now.y[i].again(); now.a[i].again(); }
+    if (V == 1 && dx && dr.thr) {
+      __syncthreads();                          // the row before has been read
+      draw_row(dr, key, base, d, num);
+      __syncthreads();
+    }
     if (!live) continue;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
@@ -216,16 +280,13 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_bwd(const T* dy, const 
       if (j >= d) continue;
       float o[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) o[e] = rs * (a[i][e] - xh[i][e] * s);
-      if (add) {
-        float t[V];
-        load_v<V>(add + base + j, t);
-#pragma unroll
-        for (int e = 0; e < V; ++e) o[e] += t[e];
+      for (int e = 0; e < V; ++e) {
+        o[e] = rs * (now.y[i][e] * gg[i][e] - now.r[i][e] * rs * s);
+        if (add) o[e] += now.a[i][e];
       }
       if (dres) store_v<V>(dres + base + j, o);
       if (dx) {
-        if (dr.thr) drop_v<V>(dr, key, base + j, o);
+        if (dr.thr) drop_v(dr, key, base, j, num, o);
         store_v<V>(dx + base + j, o);
       }
     }
@@ -255,6 +316,39 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_bwd(const T* dy, const 
   }
 }
 
+// dg[j] (+)= the sum of partial[0 .. nblk)[j]: 16 columns and 64 groups of rows a block, added in a fixed order (the 64 columns of
+// op_reduce_partials leave 12 blocks for a width of 768, each a chain of memory latencies: 6.7 us for 1024 rows).
+__global__ void __launch_bounds__(1024) k_rms_sum(const float* __restrict__ partial, int nblk, int d, float* __restrict__ dg, int accumulate) {
+  __shared__ float sh[64][17];
+  const int c = threadIdx.x & 15, q = threadIdx.x >> 4, j = blockIdx.x * 16 + c;
+  float t = 0.f;
+  if (j < d) {
+    constexpr int U = 8;
+    for (int b = q; b < nblk; b += 64 * U) {
+      float v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = b + 64 * u < nblk ? partial[(size_t)(b + 64 * u) * d + j] : 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) t += v[u];
+    }
+  }
+  sh[q][c] = t;
+  __syncthreads();
+  if (q < 8) {
+    t = 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) t += sh[8 * q + u][c];
+    sh[8 * q][c] = t;
+  }
+  __syncthreads();
+  if (q == 0 && j < d) {
+    t = 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) t += sh[8 * u][c];
+    dg[j] = accumulate ? dg[j] + t : t;
+  }
+}
+
 // Lanes and steps of a row: fn(integral constants LPR, NCH, V).
 template <int N> using Int = std::integral_constant<int, N>;
 constexpr int kMaxWidth = 16384;
@@ -268,22 +362,25 @@ hipError_t by_width(int d, bool vec, F&& fn) {
     if (d <= 1024) return fn(Int<64>(), Int<2>(), Int<8>());
     if (d <= 2048) return fn(Int<256>(), Int<1>(), Int<8>());
     if (d <= 4096) return fn(Int<256>(), Int<2>(), Int<8>());
-    if (d <= 8192) return fn(Int<256>(), Int<4>(), Int<8>());
+    if (d <= 8192) return fn(Int<1024>(), Int<1>(), Int<8>());
     return fn(Int<1024>(), Int<2>(), Int<8>());
   }
   if (d <= 64) return fn(Int<64>(), Int<1>(), Int<1>());
   if (d <= 512) return fn(Int<64>(), Int<8>(), Int<1>());
   if (d <= 2048) return fn(Int<256>(), Int<8>(), Int<1>());
+  if (d <= 8192) return fn(Int<1024>(), Int<8>(), Int<1>());
   return fn(Int<1024>(), Int<16>(), Int<1>());
 }
 template <typename... P>
 bool aligned16(P... p) { return ((((uintptr_t)p) | ...) & 15) == 0; }
 
-// Blocks of the backward kernel: enough for every compute unit to hold several, few enough for the partial sums to stay small
-// beside the tensors.
-int bwd_blocks(int rows, int rpb) {
-  const int all = (rows + rpb - 1) / rpb;
-  return all < 1024 ? all : 1024;
+// Blocks of the backward kernel: as many as the chip holds at once (four waves a SIMD), each with several rows where there are more,
+// so that the partial sums stay small beside the tensors.
+int bwd_blocks(int rows, int rpb, int lpr) {
+  const int all = (rows + rpb - 1) / rpb, most = lpr > 256 ? 256 : 1024;
+  if (all <= most) return all;
+  const int each = (all + most - 1) / most;      // the same number of rows for all
+  return (all + each - 1) / each;
 }
 
 }  // namespace
@@ -338,11 +435,13 @@ hipError_t op_rmsnorm_bwd(const OpCtx& c, const void* dy, const void* r, const f
     typedef decltype(t) T;
     return by_width(d, vec, [&](auto lpr, auto nch, auto v) {
       constexpr int L = decltype(lpr)::value, N = decltype(nch)::value, V = decltype(v)::value, th = threads_of(L), rpb = th / L;
-      const int blocks = bwd_blocks(rows, rpb);
+      const int blocks = bwd_blocks(rows, rpb, L);
       k_rms_bwd<T, L, N, V><<<blocks, th, rpb > 1 ? rpb * L * N * V * 4 : 0, c.stream>>>(
           (const T*)dy, (const T*)r, rstd, g, (const T*)add, (T*)dres, (T*)dx, dg ? c.partial : nullptr, rows, d, dr);
       const hipError_t e = hipGetLastError();
-      return e != hipSuccess || !dg ? e : op_reduce_partials(c, c.partial, blocks, d, dg, accumulate);
+      if (e != hipSuccess || !dg) return e;
+      k_rms_sum<<<(d + 15) / 16, 1024, 0, c.stream>>>(c.partial, blocks, d, dg, accumulate);
+      return hipGetLastError();
     });
   };
   return c.dt == BF16 ? go(bf16_t()) : go(float());

@@ -55,10 +55,6 @@ __device__ __forceinline__ void drop8(const Drop& d, const PhiloxKey& key, unsig
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = half_of(w, e) >= d.thr ? v[e] * d.factor : 0.f;
 }
-__device__ __forceinline__ float drop1(const Drop& d, const PhiloxKey& key, size_t i, float v) {
-  return half_of(philox(key, (unsigned)(i >> 3), d.site), (int)(i & 7)) >= d.thr ? v * d.factor : 0.f;
-}
-
 // Eight elements of either compute dtype (16-byte aligned).
 __device__ __forceinline__ void load8(const bf16_t* p, float (&v)[8]) {
   const bf16x8 t = *reinterpret_cast<const bf16x8*>(p);

@@ -127,11 +127,15 @@ def _run(name, where, *args):
     dev = where.device
     if dev.type != "cuda":
         raise KernelError(f"{name}: tensors on {dev}")
+    # the stream's handle without the object around it: 0.1 us instead of 2.9, of 8 for a call
+    stream = torch._C._cuda_getCurrentRawStream(dev.index)
     if dev.index == torch.cuda.current_device():
-        _ck(_fn(name)(*args, torch.cuda.current_stream().cuda_stream), name)
+        rc = _fn(name)(*args, stream)
     else:
         with torch.cuda.device(dev):
-            _ck(_fn(name)(*args, torch.cuda.current_stream().cuda_stream), name)
+            rc = _fn(name)(*args, stream)
+    if rc:
+        _ck(rc, name)
 
 
 def _size(t):
