@@ -288,13 +288,13 @@ struct WalkLds {
   Tile<T, DK> t[2];
   __attribute__((aligned(16))) float weight[2][kChunk];             // of whole chunks, and of the last
   int bad[2];
-  f32x4 earlier[DK <= 64 ? DK / 32 : 1][4][64];                     // two roles: as the accumulators hold it
+  f32x4 earlier[2][DK <= 64 ? DK / 32 : 1][4][64];                  // two roles, by turns: as the accumulators hold it
 };
 
 // Waves for 32 columns: two of up to 64 wide heads (64 wide, 96 heads, 1024 positions, cut: forward 17.5 us with one, 14.5 with two),
 // one of wider ones (128 wide, 1024 sequences of 1024, forward: 307 us with one, 332 with two).
 template <int DK> constexpr int kRoles = DK <= 64 ? 2 : 1;
-template <typename T, int DK> constexpr int kWavesPerSimd = DK <= 64 ? (sizeof(T) == 2 ? 4 : 3) : sizeof(T) * DK == 512 ? 1 : 2;
+template <typename T, int DK> constexpr int kWavesPerSimd = DK <= 64 ? 3 : sizeof(T) * DK == 512 ? 1 : 2;
 
 // A block: one segment of one head.
 template <typename T, int DK, bool VEC, bool FIN>
@@ -353,8 +353,8 @@ __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k
   {
     T* pad = const_cast<T*>(column<T>(job.out, at.row0, job.ldo, at.h, dh));
     const int from = first > at.len ? first : at.len;
-    for (int x = threadIdx.x; x < (at.last - from) * DK; x += NT)
-      if (x % DK < dh) pad[(size_t)(from + x / DK) * job.ldo + x % DK] = (T)0.f;
+    for (int64_t x = threadIdx.x; x < (int64_t)(at.last - from) * DK; x += NT)
+      if ((int)(x % DK) < dh) pad[(size_t)(from + x / DK) * job.ldo + x % DK] = (T)0.f;
   }
   const int rest = (stop - first) % kChunk;
   if (threadIdx.x < kChunk) {
@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k
     }
     if (!whole && job.in_scale != 1.f) scale(state, job.in_scale);
   };
-  auto earlier = [&](const Tile<T, DK>& t, float carry) {    // what the chunks before give
+  auto earlier = [&](const Tile<T, DK>& t) {                 // what the chunks before give, without its decay
     f32x16 o = (f32x16)0.f;
 #pragma unroll
     for (int kk = 0; kk < 2 * ND; ++kk) {
@@ -411,8 +411,6 @@ __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k
       split_half(state[kk / 2], kk % 2, f);
       o = mma_parts(f, frag_row<T>(&t.q[n][16 * kk + 4 * hf]), o);
     }
-#pragma unroll
-    for (int v = 0; v < 16; ++v) o[v] *= carry;
     return o;
   };
   auto own = [&](const Tile<T, DK>& t, f32x16 o, const float (&near)[16], bool slow, int c) {      // what the chunk itself adds
@@ -492,8 +490,8 @@ __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k
       }
   };
 
-  // All waves go through the same chunks with as many barriers: behind the first the chunk's tile is there, behind the second (two
-  // roles) what the earlier chunks give.  The other tile is written behind the first barrier, when nobody reads it any more.
+  // All waves go through the same chunks, a barrier each: behind it the chunk's tile is there and, two roles, what the chunks before
+  // the last one give to that one, whose output then goes out.  The other tile is written behind the barrier, when nobody reads it any more.
   if constexpr (ROLES == 1) {
     pull();
     float near[16];
@@ -504,7 +502,7 @@ __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k
       const int c = stop - u0 < kChunk ? stop - u0 : kChunk;
       __syncthreads();
       const Tile<T, DK>& t = sm.t[slot];
-      put(own(t, earlier(t, carry), near, sm.bad[slot] == u0, c), c);
+      put(own(t, earlier(t) * carry, near, sm.bad[slot] == u0, c), c);
       if (FIN || u0 + kChunk < stop) add(t, c);
       if (u0 + kChunk < stop) leave(slot ^ 1, u0 + kChunk);
     }
@@ -516,38 +514,43 @@ __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k
     for (int u0 = first, slot = 0; u0 < stop; u0 += kChunk, slot ^= 1) {
       const int c = stop - u0 < kChunk ? stop - u0 : kChunk;
       __syncthreads();
-      const f32x16 o = earlier(sm.t[slot], carry);
+      const f32x16 o = earlier(sm.t[slot]);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         f32x4 w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = o[4 * g + j];
-        sm.earlier[col][g][lane] = w;
+        sm.earlier[slot][col][g][lane] = w;
       }
-      __syncthreads();
       if (FIN || u0 + kChunk < stop) add(sm.t[slot], c);
       if (u0 + kChunk < stop) leave(slot ^ 1, u0 + kChunk);
     }
+    __syncthreads();
     finish();
   } else {
     float near[16];
     decays(near);
+    f32x16 o;                                                // of the last chunk, what it adds itself
+    auto last = [&](int slot, int c) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 w = sm.earlier[slot][col][g][lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[4 * g + j] += w[j] * carry;
+      }
+      put(o, c);
+    };
     __syncthreads();
     if (first < stop) leave(0, first);
     for (int u0 = first, slot = 0; u0 < stop; u0 += kChunk, slot ^= 1) {
       const int c = stop - u0 < kChunk ? stop - u0 : kChunk;
       __syncthreads();
-      f32x16 o = own(sm.t[slot], (f32x16)0.f, near, sm.bad[slot] == u0, c);
-      __syncthreads();
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 w = sm.earlier[col][g][lane];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[4 * g + j] += w[j];
-      }
-      put(o, c);
+      if (u0 > first) last(slot ^ 1, kChunk);
+      o = own(sm.t[slot], (f32x16)0.f, near, sm.bad[slot] == u0, c);
       if (u0 + kChunk < stop) leave(slot ^ 1, u0 + kChunk);
     }
+    __syncthreads();
+    if (first < stop) last((stop - first - 1) / kChunk & 1, (stop - first - 1) % kChunk + 1);
   }
 }
 
@@ -818,9 +821,9 @@ hipError_t states(const OpCtx& c, const StateJobs& jobs, int njobs, const Linear
 }
 
 bool shape_ok(int dt, int B, int S, int H, int dh) {
-  return (dt == F32 || dt == BF16) && B >= 0 && S >= 0 && H >= 1 && dh >= 1 && dh <= kMaxHead && (int64_t)B * H <= 65535 &&
-         (int64_t)3 * H * dh < 1 << 24 &&       // offsets inside a chunk: 24-bit rows, 32-bit bytes
-         S <= 0x7fffffff - 4 * kChunk && (int64_t)B * H * (S / kChunk + 1) <= 0x7fffffff / 32;
+  return (dt == F32 || dt == BF16) && B >= 0 && S >= 0 && S <= 1 << 30 && H >= 1 && dh >= 1 && dh <= kMaxHead &&
+         (int64_t)B * H <= 8 * 65535 &&         // grid; more than one segment a sequence only where there are few
+         (int64_t)3 * H * dh < 1 << 24;         // offsets inside a chunk: 24-bit rows, 32-bit bytes
 }
 LinearShape shape_of(const Cut& cut, const float* log_decay, const int32_t* lens, int B, int S, int H, int dh) {
   LinearShape sh;

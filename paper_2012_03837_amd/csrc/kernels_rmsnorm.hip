@@ -352,6 +352,7 @@ __global__ void __launch_bounds__(1024) k_rms_sum(const float* __restrict__ part
 // Lanes and steps of a row: fn(integral constants LPR, NCH, V).
 template <int N> using Int = std::integral_constant<int, N>;
 constexpr int kMaxWidth = 16384;
+bool shape_ok(int rows, int d) { return rows >= 0 && rows <= 1 << 30 && d >= 1 && d <= kMaxWidth && (size_t)rows * d <= (size_t)1 << 35; }
 template <typename F>
 hipError_t by_width(int d, bool vec, F&& fn) {
   if (vec) {
@@ -407,7 +408,7 @@ hipError_t op_dropout(const OpCtx& c, const void* x, const void* res, void* y, s
 hipError_t op_rmsnorm_fwd(const OpCtx& c, const void* x, const void* res, const float* g, void* r, void* y, void* y8,
                           float* y8_scale, float* rstd, int rows, int d, float eps, float p, const void* rng, unsigned site) {
   Drop dr;
-  if (rows < 0 || d < 1 || d > kMaxWidth || !make_drop(p, rng, site, &dr) || (size_t)rows * d > ((size_t)1 << 35)) return hipErrorInvalidValue;
+  if (!shape_ok(rows, d) || !make_drop(p, rng, site, &dr)) return hipErrorInvalidValue;
   if (rows == 0) return hipSuccess;
   if (!x || !g || (!y && !y8) || (y8 && !y8_scale)) return hipErrorInvalidValue;
   const bool vec = d % 8 == 0 && aligned16(x, res, g, r, y) && ((uintptr_t)y8 & 7) == 0;
@@ -426,7 +427,7 @@ hipError_t op_rmsnorm_fwd(const OpCtx& c, const void* x, const void* res, const 
 hipError_t op_rmsnorm_bwd(const OpCtx& c, const void* dy, const void* r, const float* rstd, const float* g, const void* add,
                           void* dres, void* dx, float* dg, int rows, int d, int accumulate, float p, const void* rng, unsigned site) {
   Drop dr;
-  if (rows < 0 || d < 1 || d > kMaxWidth || !make_drop(p, rng, site, &dr) || (size_t)rows * d > ((size_t)1 << 35)) return hipErrorInvalidValue;
+  if (!shape_ok(rows, d) || !make_drop(p, rng, site, &dr)) return hipErrorInvalidValue;
   if (rows == 0) return dg && !accumulate ? op_fill_f32(c, dg, d, 0.f) : hipSuccess;
   if (!dy || !r || !rstd || !g || (!dres && !dx && !dg)) return hipErrorInvalidValue;
   if (dg && (!c.partial || c.partial_elems < rmsnorm_scratch(rows, d))) return hipErrorInvalidValue;

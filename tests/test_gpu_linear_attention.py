@@ -157,6 +157,44 @@ def test_many_short_sequences_uncut(K, dtype):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
+def test_very_many_sequences(K, dtype):
+    Case(dtype, 9001, 3, 8, 8).check(K)
+
+
+def test_rows_beyond_32_bit_offsets(K):
+    """More than 2^31 elements, one sequence and a state: a decay under which only the last rows count is checked at the end, and the
+    state's gradient at the other end.  e^-3 a position: what lies 40 positions back weighs under 1e-52."""
+    import torch
+    S, H, dh, tail = 720000, 16, 64, 96
+    w = H * dh
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    qkv = torch.randn(S, 3 * w, device="cuda", generator=gen, dtype=torch.bfloat16)
+    dout = torch.randn(S, w, device="cuda", generator=gen, dtype=torch.bfloat16)
+    assert qkv.numel() > 1 << 31
+    decay = torch.full((H,), -3.0, device="cuda")
+    o, dqkv = torch.empty_like(dout), torch.empty_like(qkv)
+    s_out, ds0 = (torch.empty(1, H, dh, dh, device="cuda") for _ in range(2))
+    ws = torch.empty(max(K.lpk_linear_attention_scratch(1, S, H, dh, b) for b in (0, 1)), device="cuda")
+    K.lpk_linear_attention_fwd(1, qkv, decay, None, None, o, s_out, 1, S, H, dh, ws)
+    K.lpk_linear_attention_bwd(1, qkv, decay, None, None, dout, None, dqkv, ds0, 1, S, H, dh, ws)
+
+    def part(t, a, n, i=0):
+        return t[a:a + n, i * w:(i + 1) * w].float().cpu().numpy().astype(np.float64).reshape(1, n, H, dh).transpose(0, 2, 1, 3)
+    g = np.full(H, -3.0)
+    for a, rows in ((S - tail, slice(48, tail)), (0, slice(0, 48)), (S // 2, slice(48, 64))):
+        q, k, v, do = (part(t, a, tail, i) for t, i in ((qkv, 0), (qkv, 1), (qkv, 2), (dout, 0)))
+        ref_o, ref_s = R.linear_attention_fwd(q, k, v, g)
+        grads = R.linear_attention_bwd(q, k, v, g, do)
+        assert relerr(part(o, a, tail)[:, :, rows], ref_o[:, :, rows]) <= TOL16, a
+        for i in range(3):
+            assert relerr(part(dqkv, a, tail, i)[:, :, rows], grads[i][:, :, rows]) <= TOL16, (a, i)
+        if a == S - tail:
+            assert relerr(s_out.cpu().numpy().astype(np.float64), ref_s) <= TOL32
+        if a == 0:
+            assert relerr(ds0.cpu().numpy().astype(np.float64), grads[3]) <= TOL32
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("S,dh,lens", [(100, 64, [0, 1, 100, 64]), (700, 64, [0, 700, 129, 65]), (700, 32, [256, 257, -5, 9999]),
                                        (300, 128, [1, 192, 0, 299])])
 def test_ragged_batches(K, dtype, S, dh, lens):

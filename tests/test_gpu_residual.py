@@ -142,6 +142,19 @@ def test_dropout_under_a_replayed_graph(K):
     assert not torch.equal(seen[0], seen[1])
 
 
+def test_dropout_beyond_32_bit_offsets(K):
+    import torch
+    n = (1 << 31) + 12345
+    x = torch.ones(n, device="cuda", dtype=torch.bfloat16)
+    K.lpk_dropout(1, x, None, x, 0.25, generator(SEED, STEP), 2)
+    groups = -(-n // 8)
+    c = np.zeros((200, 4), np.uint64)
+    c[:, 0], c[:, 1], c[:, 2], c[:, 3] = np.arange(groups - 200, groups), 2, STEP & 0xFFFFFFFF, STEP >> 32
+    words = R.philox(c, (SEED & 0xFFFFFFFF, SEED >> 32))
+    kept = (np.stack([words & 0xFFFF, words >> 16], -1).reshape(-1) >= R.dropout_threshold(0.25))[:n - 8 * (groups - 200)]
+    assert np.array_equal(host(x[8 * (groups - 200):]) != 0, kept)
+
+
 # ------------------------------------------------------------------------------------------------ RMS norm
 WIDTHS = [1, 5, 8, 64, 65, 72, 128, 200, 256, 512, 513, 520, 1000, 1024, 1032, 2048, 2056, 2047, 4096, 4104, 8192, 8200, 9001, 16384]
 
@@ -265,6 +278,24 @@ def test_norm_rows_of_nothing_and_of_infinities(K, d):
     assert not got[1].any() and host(s8)[1] == 1 and not v8[1].any()
     assert np.isnan(got[3]).any() and np.isnan(host(s8)[3]) and not np.isfinite(got[2, 1])
     assert (np.abs(v8[[0, 4, 5]] - ref[[0, 2, 3]]) <= 2.0 ** -3.9 * np.abs(ref[[0, 2, 3]]) + 2.0 ** -9 * host(s8)[[0, 4, 5], None]).all()
+
+
+def test_norm_beyond_32_bit_offsets(K):
+    import torch
+    rows, d, f32 = 262400, 8200, torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(rows, d, device="cuda", generator=gen, dtype=torch.bfloat16)
+    assert x.numel() > 1 << 31
+    g, rstd, y, dg = torch.ones(d, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x), torch.empty(d, device="cuda")
+    K.lpk_rmsnorm_fwd(1, x, None, g, None, y, None, None, rstd, rows, d, 1e-5)
+    r = host(x[-2:])
+    ry, rr = R.rmsnorm_fwd(r, np.ones(d), 1e-5)
+    assert near(host(y[-2:]), ry, HALF[1], 1e-5)
+    ws = torch.empty(K.lpk_rmsnorm_scratch(rows, d), device="cuda")
+    dres = torch.empty_like(x)
+    K.lpk_rmsnorm_bwd(1, y, x, rstd, g, None, dres, None, dg, rows, d, 0, ws)
+    rdr, _ = R.rmsnorm_bwd(host(y[-2:]), r, rr, np.ones(d))
+    assert near(host(dres[-2:]), rdr, HALF[1], 1e-5 * rr.max() * np.abs(ry).max())
 
 
 def test_norm_replays(K):

@@ -33,16 +33,17 @@ DEFAULTS = {
 }
 SHAPES = [dict(dtype=2), dict(dtype=-1), dict(dh=0), dict(dh=129), dict(H=0), dict(B=-1), dict(log_decay=NULL), dict(qkv=NULL)]
 BAD = {
-    "lpk_linear_attention_fwd": SHAPES + [dict(S=-1), dict(o=NULL), dict(scratch=NULL), dict(elems=1), dict(B=65536, H=1), dict(H=1 << 30)],
+    "lpk_linear_attention_fwd": SHAPES + [dict(S=-1), dict(o=NULL), dict(scratch=NULL), dict(elems=1), dict(B=524281, H=1), dict(H=1 << 30), dict(H=87382, B=1),
+                                          dict(S=(1 << 30) + 1)],
     "lpk_linear_attention_bwd": SHAPES + [dict(S=-1), dict(dqkv=NULL), dict(dout=NULL), dict(scratch=NULL), dict(elems=1),
-                                          dict(B=1 << 15, H=3)],
+                                          dict(B=1 << 18, H=3), dict(S=(1 << 30) + 1)],
     "lpk_linear_attention_step": SHAPES + [dict(state=NULL), dict(o=NULL), dict(B=1 << 30, H=3), dict(H=1 << 30)],
     "lpk_dropout": [dict(dtype=2), dict(p=-0.1), dict(p=1.1), dict(p=NAN), dict(rng=NULL), dict(rng=P + 4), dict(x=NULL), dict(y=NULL),
                     dict(n=(1 << 35) + 1)],
-    "lpk_rmsnorm_fwd": [dict(dtype=2), dict(rows=-1), dict(d=0), dict(d=16385), dict(p=-0.1), dict(p=1.1), dict(p=NAN), dict(rng=NULL),
+    "lpk_rmsnorm_fwd": [dict(dtype=2), dict(rows=-1), dict(rows=(1 << 30) + 1, d=1), dict(d=0), dict(d=16385), dict(p=-0.1), dict(p=1.1), dict(p=NAN), dict(rng=NULL),
                         dict(rng=P + 4), dict(x=NULL), dict(g=NULL), dict(y=NULL, y8=NULL), dict(y8_scale=NULL),
                         dict(rows=1 << 30, d=64)],
-    "lpk_rmsnorm_bwd": [dict(dtype=2), dict(rows=-1), dict(d=0), dict(d=16385), dict(p=-0.1), dict(p=NAN), dict(rng=NULL), dict(dy=NULL),
+    "lpk_rmsnorm_bwd": [dict(dtype=2), dict(rows=-1), dict(rows=(1 << 30) + 1, d=1), dict(d=0), dict(d=16385), dict(p=-0.1), dict(p=NAN), dict(rng=NULL), dict(dy=NULL),
                         dict(r=NULL), dict(rstd=NULL), dict(g=NULL), dict(dres=NULL, dx=NULL, dg=NULL), dict(scratch=NULL), dict(elems=1),
                         dict(rows=1 << 30, d=64)],
 }
