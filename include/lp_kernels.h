@@ -90,10 +90,11 @@ int lpk_attention_parts(int B, int S, int H, int dh, int backward);
 /* Linear attention with a decay for each head: with l = exp(log_decay[h]) and a state S [dh, dh] per sequence and head,
  *   S_t = l S_{t-1} + k_t v_t^T,   o_t = dh^-1/2 q_t S_t      (S_{-1} = s0, zeros if null).
  * qkv [B*S, 3*H*dh] and o [B*S, H*dh] as in lpk_attention_fwd; log_decay fp32 [H] on the device, 0 or less (a constant: it has no
- * gradient); states fp32 [B, H, dh, dh].  dh up to 128, B*H up to 524280, 3*H*dh below 2^24, S up to 2^30.  lens (int32 [B] on the device, may be null: all S) are the
- * sequences' lengths, taken as 0 .. S: positions behind them are neither read nor part of a state, their rows of o and dqkv
- * become zeros.  s_out (may be null, may be s0) receives the state after the last position.  An infinity or a NaN at a position
- * reaches the outputs of that one and later ones only.
+ * gradient); states fp32 [B, H, dh, dh].  dh up to 128, B*H up to 524280, 3*H*dh below 2^24, S up to 2^30.
+ * lens (int32 [B] on the device, may be null: all S) are the sequences' lengths, taken as 0 .. S: positions behind them are neither
+ * read nor part of a state, their rows of o and dqkv become zeros.  s_out (may be null, may be s0) receives the state after the last
+ * position.  An infinity or a NaN at a position reaches, as an infinity or a NaN, the outputs of that one and later ones only (the
+ * gradients: dout's those of that position and earlier ones in dk and dv, of that one alone in dq).
  * The backward call takes the same qkv, lens and s0 with the gradients dout of o and ds_out of s_out (may be null: zeros) and
  * writes dqkv and, where it is not null, the gradient ds0 of s0.  But for s_out no output overlaps an input.
  * scratch_dev: lpk_linear_attention_scratch floats (needs no device; may be 0); contents undefined on return, so that calls which
@@ -104,7 +105,8 @@ int lpk_linear_attention_bwd(int dtype, const void* qkv, const float* log_decay,
                              const void* dout, const float* ds_out, void* dqkv, float* ds0, int B, int S, int H, int dh,
                              float* scratch_dev, size_t scratch_elems, void* stream);
 size_t lpk_linear_attention_scratch(int B, int S, int H, int dh, int backward);
-/* One position more: qkv [B, 3*H*dh], o [B, H*dh], the states are updated in place.  The same as a forward call of S = 1. */
+/* One position more: qkv [B, 3*H*dh], o [B, H*dh], the states are updated in place.  The same as a forward call of S = 1; B*H below
+ * 2^24. */
 int lpk_linear_attention_step(int dtype, const void* qkv, const float* log_decay, float* state, void* o, int B, int H, int dh,
                               void* stream);
 
@@ -117,7 +119,8 @@ int lpk_linear_attention_step(int dtype, const void* qkv, const float* log_decay
 int lpk_dropout(int dtype, const void* x, const void* res, void* y, size_t n, float p, const uint64_t* rng_dev, uint32_t site,
                 void* stream);
 
-/* Root-mean-square norm over the last dimension (d up to 16384, up to 2^30 rows, rows * d up to 2^35) behind a residual branch's dropout and addition:
+/* Root-mean-square norm over the last dimension (d up to 16384, up to 2^30 rows, rows * d up to 2^35) behind a residual branch's
+ * dropout and addition:
  *   r = drop(x) (+ res),  rstd = (mean(r^2) + eps)^-1/2,  y = r rstd g.
  * res may be null; p, rng_dev and site as in lpk_dropout (index: row * d + column; p 0: nothing is dropped).  r (may be null, may be x
  * or res) and y (compute dtype, may be null) are outputs, rstd (fp32 [rows], may be null) is kept for the backward call; the norm is

@@ -291,12 +291,16 @@ struct WalkLds {
   f32x4 earlier[2][DK <= 64 ? DK / 32 : 1][4][64];                  // two roles, by turns: as the accumulators hold it
 };
 
-// Waves for 32 columns: two of up to 64 wide heads (64 wide, 96 heads, 1024 positions, cut: forward 17.5 us with one, 14.5 with two),
-// one of wider ones (128 wide, 1024 sequences of 1024, forward: 307 us with one, 332 with two).
+// Waves for 32 columns: two of up to 64 wide heads (64 wide, 96 heads, 1024 positions, cut: 17.5 us with one, 15.1 with two),
+// one of wider ones (128 wide, 1024 heads of 1024 positions, forward: 302 us with one, 332 with two).
 template <int DK> constexpr int kRoles = DK <= 64 ? 2 : 1;
 template <typename T, int DK> constexpr int kWavesPerSimd = DK <= 64 ? 3 : sizeof(T) * DK == 512 ? 1 : 2;
 
-// A block: one segment of one head.
+// A block: one segment of one head.  bf16, a walk alone: 16 heads of 64, 16384 positions, cut, 33.8 us (134 MB of tensors, 4 TB/s); 96 heads of 1024
+// positions 15.1 us cut (3.3 TB/s), its three backward jobs uncut 51.6 (88 MB).  Where the card is full, memory bounds it (512 heads of
+// 1024 positions: forward 59 us, 4.5 TB/s); where it is not, the wave with the state, for which a chunk takes about 3000 clocks, one step waiting for
+// the other: LDS, splitting the state, products, LDS.  Two such waves with half of the rows each gained a sixth of
+// that and lost more to the wider blocks (16 heads of 16384: 52 + 98 us became 57 + 106).
 template <typename T, int DK, bool VEC, bool FIN>
 __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k_linear_walk(LinearJobs jobs, LinearShape sh, int units) {
   constexpr int ROLES = kRoles<DK>, NT = 2 * ROLES * DK, NP = sizeof(T) == 2 ? 2 : 1, NPS = sizeof(T) == 2 ? (FIN ? 3 : 2) : 1, ND = DK / 32;
@@ -567,7 +571,8 @@ struct StateJob {
 };
 struct StateJobs { StateJob j[2]; };
 
-// Two waves for every 32 columns, which take a half of every 64 positions each; their sums are added at the end.
+// Two waves for every 32 columns, which take a half of every 64 positions each; their sums are added at the end.  16 heads of 64, 16384
+// positions, bf16: 23.3 us for the 67 MB of k and v, 2.9 TB/s.
 template <typename T, int DK, bool VEC, bool FIN>
 __global__ void __launch_bounds__(4 * DK) k_linear_states(StateJobs jobs, LinearShape sh, int units) {
   constexpr int NPS = sizeof(T) == 2 ? (FIN ? 3 : 2) : 1, ND = DK / 32, LD = DK + kPad<T>, R = 2 * kChunk;
@@ -652,7 +657,8 @@ constexpr int state_lds() {
   return tiles > sums ? tiles : sums;
 }
 
-// In place: what a segment adds becomes the state before it.  A thread takes V neighbouring elements of the state.
+// In place: what a segment adds becomes the state before it.  A thread takes V neighbouring elements of the state:
+// a chain of one multiplication and addition a segment, so that the loads in flight bound it (47 segments of 16 heads of 64: 9.1 us, 25 MB).
 template <int V>
 __global__ void __launch_bounds__(256) k_linear_scan(StateJobs jobs, LinearShape sh) {
   typedef __attribute__((ext_vector_type(V))) float FV;
@@ -687,7 +693,9 @@ __global__ void __launch_bounds__(256) k_linear_scan(StateJobs jobs, LinearShape
   if (job.fin) *reinterpret_cast<FV*>(job.fin + (size_t)bh * dd + x) = s * job.out_scale;
 }
 
-// One position: the state is read, decayed, added to and written back; a wave takes `rows` of its rows at a time.
+// One position, a block for each head: the state is read, decayed, added to and written back in one pass, four neighbouring elements a thread and
+// four rows of them in flight.  Bound by the state's bytes (3072 heads of 64, bf16: 16.9 us for 101 MB, of which the last-level cache holds a part:
+// 6 TB/s), with few heads by the launch (12 heads: 3.6 us).
 template <typename T>
 __global__ void __launch_bounds__(256) k_linear_step(const T* __restrict__ qkv, const float* __restrict__ log_decay, float* __restrict__ state,
                                                      T* __restrict__ o, int H, int dh, float scale) {
@@ -747,9 +755,10 @@ __global__ void __launch_bounds__(256) k_linear_step(const T* __restrict__ qkv, 
 constexpr int kMaxHead = 128;
 
 // Segments of a sequence: as many as give 768 blocks, three or so for each compute unit, but none of less than four chunks, and
-// no cut into two, which costs two more launches and a second pass over k and v.  (Forward and backward, us: 96 heads of 64, 1024 positions,
-// for 384 / 768 / 1536 blocks 33 + 53, 32 + 54, 32 + 59; 16 heads, 16384 positions 61 + 135, 56 + 103, 66 + 112.  Of two chunks:
-// 32 heads in fp32, 2048 positions 62 + 95 instead of 47 + 95.  In two: 8 heads, 300 positions 18 + 19, uncut 15 + 15.)
+// no cut into two, which costs two more launches and a second pass over k and v.  (Forward and backward, us: 16 heads of 64, 16384 positions, for
+// 384 / 768 / 1024 blocks 57 + 127, 54 + 100, 60 + 117; 96 heads, 1024 positions 31 + 48, 31 + 49, 31 + 53.  Four chunks at least, or two: 32 heads in
+// fp32, 2048 positions, forward 42 and 55; or six: 35 heads in fp32, 511 positions, which are then not cut, forward 25 and 42.  In two: 8 heads, 300
+// positions 16 + 17, uncut 14 + 14.)
 struct Cut { int segments, per; };
 Cut cut_of(int B, int S, int H, int jobs) {
   const int chunks = (S + kChunk - 1) / kChunk;
@@ -923,7 +932,7 @@ hipError_t op_linear_attn_bwd(const OpCtx& c, const void* qkv, const float* log_
 
 hipError_t op_linear_attn_step(const OpCtx& c, const void* qkv, const float* log_decay, float* state, void* o, int B, int H, int dh) {
   ProfScope prof_(c, KC_ATTN_FWD);
-  if ((c.dt != F32 && c.dt != BF16) || B < 0 || H < 1 || dh < 1 || dh > kMaxHead || (int64_t)B * H > 0x7fffffff ||
+  if ((c.dt != F32 && c.dt != BF16) || B < 0 || H < 1 || dh < 1 || dh > kMaxHead || (int64_t)B * H >= 1 << 24 ||
       (int64_t)3 * H * dh > 0x7fffffff) return hipErrorInvalidValue;
   if (B == 0) return hipSuccess;
   if (!qkv || !log_decay || !state || !o) return hipErrorInvalidValue;

@@ -389,3 +389,35 @@ def test_two_streams_at_once(K):
         ref = c.reference()
         for n in ("o", "dqkv"):
             assert relerr(c.d[n].float().cpu().numpy().astype(np.float64), ref[n]) <= TOL16
+
+
+@pytest.mark.parametrize("S,dh,lens", [(70, 64, [70, 33]), (600, 32, None), (100, 128, None)])
+def test_gradients_against_differences(K, S, dh, lens):
+    """loss = <dout, o> + <ds_out, s_out> is linear in each of q, k, v and s0: its change over a whole step along one of them is the
+    gradient's product with the step, but for the 3e-6 by which outputs and gradients are off."""
+    import torch
+    c = Case(0, 2, S, 2, dh, seed=S, lens=lens)
+    c.upload()
+    d = c.outputs()
+    w = 2 * dh
+
+    def loss():
+        c.forward(K)
+        o, s = (d[n].double().cpu().numpy().ravel() for n in ("o", "s_out"))
+        a, b = c.dout.astype(np.float64).ravel(), c.ds_out.astype(np.float64).ravel()
+        return a @ o + b @ s, 3e-6 * (np.linalg.norm(a) * np.linalg.norm(o) + np.linalg.norm(b) * np.linalg.norm(s))
+
+    c.backward(K)
+    grads = {i: d["dqkv"][:, i * w:(i + 1) * w].double().cpu().numpy() for i in range(3)} | {3: d["ds0"].double().cpu().numpy()}
+    rng = np.random.default_rng(dh)
+    base, off = loss()
+    for i in range(4):
+        at = d["s0"] if i == 3 else d["qkv"][:, i * w:(i + 1) * w]
+        was = at.clone()
+        at.add_(torch.from_numpy(rng.standard_normal(tuple(at.shape)).astype(np.float32)).cuda())
+        step = (at.double() - was.double()).cpu().numpy()
+        moved, off2 = loss()
+        at.copy_(was)
+        expect = float((grads[i] * step).sum())
+        assert abs(moved - base - expect) <= off + off2 + 3e-6 * np.linalg.norm(grads[i]) * np.linalg.norm(step), "qkvs"[i]
+        assert abs(expect) > 10 * (off + off2)              # the step is no smaller than what it is measured with

@@ -393,3 +393,60 @@ def test_attention_branch_of_a_layer(K, dtype):
         a, c = host(got), want.detach().numpy()
         assert np.linalg.norm(a - c) <= tol * np.linalg.norm(c), (name, np.linalg.norm(a - c) / np.linalg.norm(c))
     assert b.guards_stand()
+
+
+@pytest.mark.parametrize("d", [64, 100, 1024])
+def test_norm_gradients_against_differences(K, d):
+    """loss = <dy, y> + <add, r> with dropout and residual.  Along a step t e of x, r moves on a line with the direction drop(e), and r / |r| on
+    a circle whose angle has the derivatives |e| / c, |e|^2 / c^2 and 2 |e|^3 / c^3 at most, c the line's distance from 0: the third derivative of r / |r| is
+    at most 2 + 3 + 1 times (|e| / c)^3, and a central difference is off by t^2 / 6 of that.  y and r are off by 2^-24 (8 + sqrt d) of
+    the row's largest value, the gradients by as much."""
+    import torch
+    rows, eps, p, t = 40, 1e-5, 0.3, 2.0 ** -5
+    b = Bench(0, d)
+    x, res, dy, add, e = (b.rnd(rows, d) for _ in range(5))
+    g = (1 + 0.2 * b.rng.standard_normal(d)).astype(np.float32)
+    rng, f32 = generator(SEED, STEP), torch.float32
+    dev = {n: b.dev(a) for n, a in dict(x=x, res=res, dy=dy, add=add, g=g).items()}
+    r, y, dres, dx = (b.room((rows, d)) for _ in range(4))
+    rstd, dg = b.room((rows,)), b.room((d,))
+    unit = 2.0 ** -24 * (8 + np.sqrt(d))
+
+    def loss(at, gain):
+        K.lpk_rmsnorm_fwd(0, at, dev["res"], gain, r, y, None, None, rstd, rows, d, eps, p, rng, 3)
+        yh, rh = host(y), host(r)
+        off = unit * ((np.abs(dy).sum(1) * np.abs(yh).max(1)).sum() + (np.abs(add).sum(1) * np.abs(rh).max(1)).sum())
+        return (dy.astype(np.float64) * yh).sum() + (add.astype(np.float64) * rh).sum(), off
+
+    base, off0 = loss(dev["x"], dev["g"])
+    rh = host(r)
+    K.lpk_rmsnorm_bwd(0, dev["dy"], r, rstd, dev["g"], dev["add"], dres, dx, dg, rows, d, 0,
+                      torch.empty(K.lpk_rmsnorm_scratch(rows, d), device="cuda", dtype=f32), p, rng, 3)
+    dxh, dgh = host(dx), host(dg)
+    # x
+    high, low = (b.dev((x + s * t * e).astype(np.float32)) for s in (1, -1))
+    step = host(high) - host(low)                            # 2 t e, as rounded
+    (a, offa), (c, offc) = loss(high, dev["g"]), loss(low, dev["g"])
+    along = np.linalg.norm(R.dropout(step, p, SEED, STEP, 3), axis=1) / 2
+    clear = np.linalg.norm(rh, axis=1) - along
+    assert (clear > 0).all()
+    curve = 2 * (np.linalg.norm(g * dy, axis=1) * np.sqrt(d) * (along / clear) ** 3).sum()
+    # <dxh, step>: gradients off by `unit` of their row's largest term
+    slack = unit * (np.abs(dxh).max(1) * np.abs(step).sum(1)).sum()
+    assert abs(a - c - (dxh * step).sum()) <= curve + offa + offc + slack
+    # g: the loss is linear in it
+    moved = b.dev((2 * g).astype(np.float32))
+    (a, offa) = loss(dev["x"], moved)
+    assert abs(a - base - (dgh * g).sum()) <= offa + off0 + unit * (np.abs(dy) * np.abs(host(y))).sum()
+
+
+def test_norm_of_very_many_rows(K):
+    """More rows than a launch has threads for along one axis."""
+    import torch
+    rows = (1 << 26) + 5
+    x = torch.arange(rows, device="cuda", dtype=torch.int32).remainder_(97).sub_(48).float()
+    g, y = torch.full((1,), 2.0, device="cuda"), torch.full((rows + 64,), 7.0, device="cuda")
+    K.lpk_rmsnorm_fwd(0, x, None, g, None, y, None, None, None, rows, 1, 1e-5)
+    # five operations in fp32, each off by half a unit
+    assert bool((y[:rows].double() - 2 * x.double() / (x.double() ** 2 + 1e-5).sqrt()).abs().max() <= 5 * 2.0 ** -24 * 2)
+    assert bool((y[rows:] == 7).all())

@@ -37,7 +37,7 @@ BAD = {
                                           dict(S=(1 << 30) + 1)],
     "lpk_linear_attention_bwd": SHAPES + [dict(S=-1), dict(dqkv=NULL), dict(dout=NULL), dict(scratch=NULL), dict(elems=1),
                                           dict(B=1 << 18, H=3), dict(S=(1 << 30) + 1)],
-    "lpk_linear_attention_step": SHAPES + [dict(state=NULL), dict(o=NULL), dict(B=1 << 30, H=3), dict(H=1 << 30)],
+    "lpk_linear_attention_step": SHAPES + [dict(state=NULL), dict(o=NULL), dict(B=1 << 30, H=3), dict(H=1 << 30), dict(B=1 << 24, H=1, dh=1)],
     "lpk_dropout": [dict(dtype=2), dict(p=-0.1), dict(p=1.1), dict(p=NAN), dict(rng=NULL), dict(rng=P + 4), dict(x=NULL), dict(y=NULL),
                     dict(n=(1 << 35) + 1)],
     "lpk_rmsnorm_fwd": [dict(dtype=2), dict(rows=-1), dict(rows=(1 << 30) + 1, d=1), dict(d=0), dict(d=16385), dict(p=-0.1), dict(p=1.1), dict(p=NAN), dict(rng=NULL),
