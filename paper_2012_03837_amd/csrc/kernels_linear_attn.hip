@@ -280,9 +280,13 @@ __device__ __forceinline__ void scale(f32x16 (&state)[ND], float by) {
     for (int v = 0; v < 16; ++v) state[i][v] *= by;
 }
 
+// Between the rows of a tile: 16 bytes spread what a wave reads of 32 neighbouring rows or of 4 rows, 64 bytes each, over the banks,
+// but for 128 bf16, which are the banks' period (the walk there, 32 heads of 2048 positions, forward and backward: 50 + 88 us with 16 bytes, 49 + 86 with
+// 80; its states kernel, whose blocks hold twice the rows, loses by them, 53 + 91).
 template <typename T> constexpr int kPad = 16 / (int)sizeof(T);
+template <typename T, int DK> constexpr int kWalkPad = sizeof(T) == 2 && DK == 128 ? 40 : kPad<T>;
 template <typename T, int DK>
-struct Tile { __attribute__((aligned(16))) T q[kChunk][DK + kPad<T>], k[kChunk][DK + kPad<T>], v[kChunk][DK + kPad<T>]; };
+struct Tile { __attribute__((aligned(16))) T q[kChunk][DK + kWalkPad<T, DK>], k[kChunk][DK + kWalkPad<T, DK>], v[kChunk][DK + kWalkPad<T, DK>]; };
 template <typename T, int DK>
 struct WalkLds {
   Tile<T, DK> t[2];
@@ -292,19 +296,19 @@ struct WalkLds {
 };
 
 // Waves for 32 columns: two of up to 64 wide heads (64 wide, 96 heads, 1024 positions, cut: 17.5 us with one, 15.1 with two),
-// one of wider ones (128 wide, 1024 heads of 1024 positions, forward: 302 us with one, 332 with two).
+// one of wider ones (128 wide, 1024 heads of 1024 positions, forward: 300 us with one, 332 with two).
 template <int DK> constexpr int kRoles = DK <= 64 ? 2 : 1;
 template <typename T, int DK> constexpr int kWavesPerSimd = DK <= 64 ? 3 : sizeof(T) * DK == 512 ? 1 : 2;
 
 // A block: one segment of one head.  bf16, a walk alone: 16 heads of 64, 16384 positions, cut, 33.8 us (134 MB of tensors, 4 TB/s); 96 heads of 1024
 // positions 15.1 us cut (3.3 TB/s), its three backward jobs uncut 51.6 (88 MB).  Where the card is full, memory bounds it (512 heads of
-// 1024 positions: forward 59 us, 4.5 TB/s); where it is not, the wave with the state, for which a chunk takes about 3000 clocks, one step waiting for
+// 1024 positions: forward 60 us, 4.4 TB/s); where it is not, the wave with the state, for which a chunk takes about 3000 clocks, one step waiting for
 // the other: LDS, splitting the state, products, LDS.  Two such waves with half of the rows each gained a sixth of
 // that and lost more to the wider blocks (16 heads of 16384: 52 + 98 us became 57 + 106).
 template <typename T, int DK, bool VEC, bool FIN>
 __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k_linear_walk(LinearJobs jobs, LinearShape sh, int units) {
   constexpr int ROLES = kRoles<DK>, NT = 2 * ROLES * DK, NP = sizeof(T) == 2 ? 2 : 1, NPS = sizeof(T) == 2 ? (FIN ? 3 : 2) : 1, ND = DK / 32;
-  constexpr int LD = DK + kPad<T>;
+  constexpr int LD = DK + kWalkPad<T, DK>;
   typedef typename Frag<T>::V FV;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   WalkLds<T, DK>& sm = *reinterpret_cast<WalkLds<T, DK>*>(smem);
@@ -754,16 +758,20 @@ __global__ void __launch_bounds__(256) k_linear_step(const T* __restrict__ qkv, 
 
 constexpr int kMaxHead = 128;
 
-// Segments of a sequence: as many as give 768 blocks, three or so for each compute unit, but none of less than four chunks, and
-// no cut into two, which costs two more launches and a second pass over k and v.  (Forward and backward, us: 16 heads of 64, 16384 positions, for
-// 384 / 768 / 1024 blocks 57 + 127, 54 + 100, 60 + 117; 96 heads, 1024 positions 31 + 48, 31 + 49, 31 + 53.  Four chunks at least, or two: 32 heads in
-// fp32, 2048 positions, forward 42 and 55; or six: 35 heads in fp32, 511 positions, which are then not cut, forward 25 and 42.  In two: 8 heads, 300
-// positions 16 + 17, uncut 14 + 14.)
+// Segments of a sequence: as many as make one round of the blocks that run at once (three a compute unit up to 64 wide, two of wider heads, one in
+// fp32 beyond 96, whose registers hold no second one; there two rounds where one would be less than three segments), but none of less than four chunks, and no
+// cut into two, which costs two more launches and a second pass over k and v.  Forward and backward, us:
+//   16 heads of 64, 16384 positions, for 384 / 768 / 1024 blocks     57 + 127, 54 + 100, 60 + 117;  96 heads, 1024 positions  31 + 48, 31 + 49, 31 + 53
+//   32 heads of 128, 2048 positions, for 256 / 512 / 768 blocks      49 + 156, 52 + 83, 50 + 86;    128 heads  162 + 249, 115 + 250, 137 + 250
+//   the same in fp32, 40 heads 134 + 507, 153 + 355, 168 + 351;      80 heads  251 + 518, 267 + 518, 296 + 663
+//   of four chunks at least, or two: 32 heads of 64 in fp32, 2048 positions, forward 42 and 55; or six: 35 heads in fp32, 511 positions, which are
+//   then not cut, 25 and 42;  in two: 8 heads of 64, 300 positions 16 + 17, uncut 14 + 14
 struct Cut { int segments, per; };
-Cut cut_of(int B, int S, int H, int jobs) {
-  const int chunks = (S + kChunk - 1) / kChunk;
-  const long blocks = (long)B * H * jobs;
-  long want = blocks > 0 ? 768 / blocks : 1;
+Cut cut_of(int dt, int B, int S, int H, int dh, int jobs) {
+  const int chunks = (S + kChunk - 1) / kChunk, alone = dt == F32 && dh > 96;
+  const long blocks = (long)B * H * jobs, once = 256 * (dh <= 64 ? 3 : alone ? 1 : 2);
+  long want = blocks > 0 ? once / blocks : 1;
+  if (alone && want < 3) want = 2 * once / blocks;
   const long most = chunks / 4;
   if (want > most) want = most;
   if (want < 3) want = 1;
@@ -771,6 +779,10 @@ Cut cut_of(int B, int S, int H, int jobs) {
   c.per = chunks > 0 ? (int)((chunks + want - 1) / want) : 1;
   c.segments = chunks > 0 ? (chunks + c.per - 1) / c.per : 1;
   return c;
+}
+
+size_t cut_elems(const Cut& c, int B, int H, int dh, bool backward) {
+  return c.segments > 1 ? (size_t)B * H * c.segments * dh * dh * (backward ? 2 : 1) : 0;
 }
 
 // Calls fn(integral DK, bool VEC) for a head size.
@@ -851,9 +863,10 @@ bool whole_chunks(int dh, std::initializer_list<const void*> bufs) {
 }  // namespace
 
 size_t linear_attn_scratch(int B, int S, int H, int dh, bool backward) {
-  if (!shape_ok(BF16, B, S, H, dh)) return 0;
-  const Cut cut = cut_of(B, S, H, backward ? 3 : 1);
-  return cut.segments > 1 ? (size_t)B * H * cut.segments * dh * dh * (backward ? 2 : 1) : 0;
+  size_t n = 0;
+  for (int dt : {F32, BF16})                     // enough for either compute dtype
+    if (shape_ok(dt, B, S, H, dh)) n = std::max(n, cut_elems(cut_of(dt, B, S, H, dh, backward ? 3 : 1), B, H, dh, backward));
+  return n;
 }
 
 hipError_t op_linear_attn_fwd(const OpCtx& c, const void* qkv, const float* log_decay, const int32_t* lens, const float* s0, void* o,
@@ -862,8 +875,8 @@ hipError_t op_linear_attn_fwd(const OpCtx& c, const void* qkv, const float* log_
   if (!shape_ok(c.dt, B, S, H, dh)) return hipErrorInvalidValue;
   if (B == 0) return hipSuccess;
   if (!log_decay || (S > 0 && (!qkv || !o))) return hipErrorInvalidValue;
-  const Cut cut = cut_of(B, S, H, 1);
-  if (cut.segments > 1 && (!c.partial || c.partial_elems < linear_attn_scratch(B, S, H, dh, false))) return hipErrorInvalidValue;
+  const Cut cut = cut_of(c.dt, B, S, H, dh, 1);
+  if (cut.segments > 1 && (!c.partial || c.partial_elems < cut_elems(cut, B, H, dh, false))) return hipErrorInvalidValue;
   const LinearShape sh = shape_of(cut, log_decay, lens, B, S, H, dh);
   const bool vec = whole_chunks(dh, {qkv, o});
   const size_t e = dtype_size(c.dt);
@@ -892,8 +905,8 @@ hipError_t op_linear_attn_bwd(const OpCtx& c, const void* qkv, const float* log_
   if (!shape_ok(c.dt, B, S, H, dh)) return hipErrorInvalidValue;
   if (B == 0) return hipSuccess;
   if (!log_decay || (S > 0 && (!qkv || !dout || !dqkv))) return hipErrorInvalidValue;
-  const Cut cut = cut_of(B, S, H, 3);
-  if (cut.segments > 1 && (!c.partial || c.partial_elems < linear_attn_scratch(B, S, H, dh, true))) return hipErrorInvalidValue;
+  const Cut cut = cut_of(c.dt, B, S, H, dh, 3);
+  if (cut.segments > 1 && (!c.partial || c.partial_elems < cut_elems(cut, B, H, dh, true))) return hipErrorInvalidValue;
   const LinearShape sh = shape_of(cut, log_decay, lens, B, S, H, dh);
   const bool vec = whole_chunks(dh, {qkv, dout, dqkv});
   const size_t e = dtype_size(c.dt);
