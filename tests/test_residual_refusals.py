@@ -75,3 +75,25 @@ def test_wrappers_want_device_tensors(K):
     x = torch.zeros(8)
     with pytest.raises(K.KernelError):
         K.lpk_dropout(0, x, None, x, 0.0, None, 0)
+
+
+@pytest.mark.gpu
+def test_wrappers_refuse_what_the_kernels_would_misread(K):
+    """Lengths of 64 bits, a strided view, another element size, a host tensor: refused before anything is launched."""
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    qkv, o = torch.zeros(20, 3 * 64, device="cuda"), torch.zeros(20, 64, device="cuda")
+    decay = torch.zeros(1, device="cuda")
+
+    def run(qkv=qkv, decay=decay, lens=None, o=o, dtype=0):
+        K.lpk_linear_attention_fwd(dtype, qkv, decay, lens, None, o, None, 2, 10, 1, 64)
+
+    run(lens=torch.tensor([3, 4], device="cuda", dtype=torch.int32))
+    for bad in (dict(lens=torch.tensor([3, 4], device="cuda")), dict(lens=torch.tensor([3, 4], dtype=torch.int32)), dict(decay=decay.double()),
+                dict(qkv=torch.zeros(3 * 64, 20, device="cuda").t()), dict(qkv=qkv.bfloat16()), dict(o=o.bfloat16()), dict(dtype=1)):
+        with pytest.raises(K.KernelError):
+            run(**bad)
+    x = torch.zeros(64, device="cuda")
+    with pytest.raises(K.KernelError):
+        K.lpk_dropout(0, x, None, x, 0.5, torch.zeros(2, device="cuda", dtype=torch.int32), 0)
