@@ -698,7 +698,7 @@ __global__ void __launch_bounds__(256) k_linear_scan(StateJobs jobs, LinearShape
 }
 
 // One position, a block for each head: the state is read, decayed, added to and written back in one pass, four neighbouring elements a thread and
-// four rows of them in flight.  Bound by the state's bytes (3072 heads of 64, bf16: 16.9 us for 101 MB, of which the last-level cache holds a part:
+// four rows of them in flight.  Bound by the state's bytes (192 sequences of 16 heads of 64, bf16: 16.8 us for 101 MB, of which the last-level cache holds a part:
 // 6 TB/s), with few heads by the launch (12 heads: 3.6 us).
 template <typename T>
 __global__ void __launch_bounds__(256) k_linear_step(const T* __restrict__ qkv, const float* __restrict__ log_decay, float* __restrict__ state,

@@ -4,8 +4,8 @@
 //   backward:  a = g dy,  dres = rstd (a - r rstd^2 mean(a r)) (+ add),  dx = drop'(dres),  dg = sum over rows of dy r rstd
 // All are bound by memory: every tensor is read or written once, 16 bytes a lane, with the row in registers between its sums and
 // its outputs.  A row belongs to LPR neighbouring lanes (8 to 64: rows of up to 512 elements fill a wave with several of them, as
-// the norm over a head needs) or to a block of 256 or 1024 threads.  V = 8 elements a lane and step, one where a width or an
-// address does not allow that.
+// the norm over a head needs) or to a block of 256 to 1024 threads.  Eight neighbouring elements a lane and step; where the
+// width or an address is no multiple of them (ODD) the same accesses stand anywhere and a row's last ones are taken singly.
 // What they take, bf16 (tensors' bytes over the time; 8192 rows of 4096 are 67 MB a tensor):
 //   dropout and addition, 8192 x 4096, and its gradient   63.9 us, 5.2 TB/s (335 MB)
 //   forward, dropout, addition, 8192 x 768                13.9 us, 3.6 TB/s; with 8-bit output, 8192 x 4096, 46.4 us, 5.1 TB/s
@@ -66,11 +66,27 @@ __device__ __forceinline__ float row_all(float v, float* sh) {
   }
   return v;
 }
-// V elements as they stand in memory: loads that are asked for long before they are used.
-template <typename T, int V> struct Raw;
-template <> struct Raw<bf16_t, 8> {
+// Eight elements as they stand in memory: loads that are asked for long before they are used.  ODD: on no boundary but an element's, and
+// only the first n of them there (the others are zeros); 16 bytes may be loaded from anywhere.  bf16, dropout and addition, forward, with an
+// element a lane and so: 16000 rows of 1001 39 and 25 us (5.1 TB/s), 37000 of 449 42 and 26, 100000 of 65 45 and 16; backward 41 and 32, 37 and 43,
+// 50 and 29.
+template <typename T> struct Raw;
+template <> struct Raw<bf16_t> {
+  typedef bf16x8 __attribute__((aligned(2))) Anywhere;
   bf16x8 a;
-  __device__ __forceinline__ void load(const bf16_t* p) { a = *reinterpret_cast<const bf16x8*>(p); }
+  template <bool ODD> __device__ __forceinline__ void load(const bf16_t* p, int n) {
+    if (!ODD) {
+      a = *reinterpret_cast<const bf16x8*>(p);
+    } else if (n >= 8) {
+      a = *reinterpret_cast<const Anywhere*>(p);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e) {
+        const bf16_t x = p[e < n ? e : 0];      // all under way at once; in branches, as fp32 has them, each waits for the half before it
+        a[e] = e < n ? x : (bf16_t)0.f;
+      }
+    }
+  }
   __device__ __forceinline__ void zero() { a = (bf16x8)(bf16_t)0.f; }
   __device__ __forceinline__ float operator[](int e) const { return (float)a[e]; }
   // what has been computed from it so far is not kept in registers (a conversion costs less than twice the registers)
@@ -81,90 +97,124 @@ template <> struct Raw<bf16_t, 8> {
     a = __builtin_bit_cast(bf16x8, w);
   }
 };
-template <> struct Raw<float, 8> {
+template <> struct Raw<float> {
+  typedef f32x4 __attribute__((aligned(4))) Anywhere;
   f32x4 a, b;
-  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const f32x4*>(p); b = *reinterpret_cast<const f32x4*>(p + 4); }
+  template <bool ODD> __device__ __forceinline__ void load(const float* p, int n) {
+    if (!ODD) {
+      a = *reinterpret_cast<const f32x4*>(p);
+      b = *reinterpret_cast<const f32x4*>(p + 4);
+    } else if (n >= 8) {
+      a = *reinterpret_cast<const Anywhere*>(p);
+      b = *reinterpret_cast<const Anywhere*>(p + 4);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (e < n) a[e] = p[e];
+        if (4 + e < n) b[e] = p[4 + e];
+      }
+    }
+  }
   __device__ __forceinline__ void zero() { a = (f32x4)0.f; b = (f32x4)0.f; }
   __device__ __forceinline__ float operator[](int e) const { return e < 4 ? a[e] : b[e - 4]; }
   __device__ __forceinline__ void again() { asm volatile("" : "+v"(a), "+v"(b)); }
 };
-template <typename T> struct Raw<T, 1> {
-  T a;
-  __device__ __forceinline__ void load(const T* p) { a = *p; }
-  __device__ __forceinline__ void zero() { a = (T)0.f; }
-  __device__ __forceinline__ float operator[](int) const { return to_f(a); }
-  __device__ __forceinline__ void again() {}
-};
-template <int V, typename T>
-__device__ __forceinline__ void store_v(T* p, const float (&v)[V]) {
-  if constexpr (V == 8) store8(p, v);
-  else *p = from_f<T>(v[0]);
+template <bool ODD>
+__device__ __forceinline__ void store_n(bf16_t* p, const float (&v)[8], int n) {
+  if (!ODD) {
+    store8(p, v);
+  } else if (n >= 8) {
+    bf16x8 t;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = (bf16_t)v[e];
+    *reinterpret_cast<Raw<bf16_t>::Anywhere*>(p) = t;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (e < n) p[e] = (bf16_t)v[e];
+  }
 }
-// One element a lane: eight neighbours would draw the same four words.  The lanes of a row draw them once, a counter each, and
-// leave them in LDS, where element j's number stands at (first & 7) + j.  (37000 rows of 449, bf16: forward 58 us
-// with every lane's own words, 39 so; backward 60 and 37.)
-template <int LPR, int NCH> struct Numbers { uint4 w[LPR * NCH / 8 + 2]; };
+template <bool ODD>
+__device__ __forceinline__ void store_n(float* p, const float (&v)[8], int n) {
+  if (!ODD) {
+    store8(p, v);
+  } else if (n >= 8) {
+    *reinterpret_cast<Raw<float>::Anywhere*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<Raw<float>::Anywhere*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (e < n) p[e] = v[e];
+  }
+}
+// A row that begins inside a group of eight would draw every group twice.  Its lanes draw them once, a counter each, and
+// leave them in LDS, where element j's number stands at (first & 7) + j.
+template <int LPR, int NCH> struct Numbers { uint4 w[LPR * NCH + 2]; };
 template <int LPR, int NCH>
 __device__ __forceinline__ void draw_row(const Drop& d, const PhiloxKey& key, size_t first, int width, Numbers<LPR, NCH>& num) {
   const int groups = ((int)(first & 7) + width + 7) >> 3;
   for (int k = threadIdx.x % LPR; k < groups; k += LPR) num.w[k] = philox(key, (unsigned)(first >> 3) + k, d.site);
 }
-template <int LPR, int NCH, int V>
-__device__ __forceinline__ void drop_v(const Drop& d, const PhiloxKey& key, size_t first, int j, const Numbers<LPR, NCH>& num, float (&v)[V]) {
-  if constexpr (V == 8) drop8(d, key, (unsigned)((first + j) >> 3), v);
-  else v[0] = reinterpret_cast<const unsigned short*>(num.w)[(first & 7) + j] >= d.thr ? v[0] * d.factor : 0.f;
-}
-__device__ __forceinline__ unsigned char to_e4m3(float a) {
-  return (unsigned char)(__builtin_amdgcn_cvt_pk_fp8_f32(a, a, 0, false) & 0xff);
+template <bool ODD, int LPR, int NCH>
+__device__ __forceinline__ void drop_row(const Drop& d, const PhiloxKey& key, size_t first, int j, const Numbers<LPR, NCH>& num, float (&v)[8]) {
+  if constexpr (!ODD) {
+    drop8(d, key, (unsigned)((first + j) >> 3), v);
+  } else {
+    const unsigned short* u = reinterpret_cast<const unsigned short*>(num.w) + (first & 7) + j;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = u[e] >= d.thr ? v[e] * d.factor : 0.f;
+  }
 }
 
 constexpr int threads_of(int LPR) { return LPR > 256 ? LPR : 256; }
 
-template <typename T, int LPR, int NCH, int V>
+template <typename T, int LPR, int NCH, bool ODD>
 __global__ void __launch_bounds__(threads_of(LPR)) k_rms_fwd(const T* x, const T* res, const float* __restrict__ g, T* r, T* y,
                                                              unsigned char* __restrict__ y8, float* __restrict__ y8_scale,
                                                              float* __restrict__ rstd, int rows, int d, float eps, Drop dr) {
   __shared__ float sh[16];
   constexpr int RPB = threads_of(LPR) / LPR;
-  __shared__ Numbers<LPR, V == 1 ? NCH : 0> numbers[RPB];
+  __shared__ Numbers<ODD ? LPR : 0, ODD ? NCH : 0> numbers[RPB];
   auto& num = numbers[threadIdx.x / LPR];
   const int lane = threadIdx.x % LPR, row = (blockIdx.y * gridDim.x + blockIdx.x) * RPB + threadIdx.x / LPR;
   const bool live = row < rows;                 // rows share a wave: those past the end go along in its shuffles
   const size_t base = (size_t)row * d;
   const int d_live = live ? d : 0;
-  Raw<T, V> xr[NCH], rr[NCH];
-  Raw<float, V> gr[NCH];
+  Raw<T> xr[NCH], rr[NCH];
+  Raw<float> gr[NCH];
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
-    const int j = (lane + LPR * i) * V;
+    const int j = (lane + LPR * i) * 8;
     xr[i].zero();
     rr[i].zero();
     gr[i].zero();
     if (j < d_live) {
-      xr[i].load(x + base + j);
-      if (res) rr[i].load(res + base + j);
-      gr[i].load(g + j);
+      xr[i].template load<ODD>(x + base + j, d - j);
+      if (res) rr[i].template load<ODD>(res + base + j, d - j);
+      gr[i].template load<ODD>(g + j, d - j);
     }
   }
   const PhiloxKey key = philox_key(dr);
-  if (V == 1 && dr.thr) {
-    draw_row(dr, key, base, d, num);
-    __syncthreads();
+  if constexpr (ODD) {
+    if (dr.thr) {
+      draw_row(dr, key, base, d, num);
+      __syncthreads();
+    }
   }
-  float v[NCH][V], s = 0.f;
+  float v[NCH][8], s = 0.f;
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
-    const int j = (lane + LPR * i) * V;
+    const int j = (lane + LPR * i) * 8;
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[i][e] = xr[i][e];
-    if (dr.thr && (V == 8 || j < d)) drop_v(dr, key, base, j, num, v[i]);
+    for (int e = 0; e < 8; ++e) v[i][e] = xr[i][e];
+    if (dr.thr && (!ODD || j < d)) drop_row<ODD>(dr, key, base, j, num, v[i]);
     if (res) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[i][e] += rr[i][e];
+      for (int e = 0; e < 8; ++e) v[i][e] += rr[i][e];
     }
-    if (r && j < d_live) store_v<V>(r + base + j, v[i]);
+    if (r && j < d_live) store_n<ODD>(r + base + j, v[i], d - j);
 #pragma unroll
-    for (int e = 0; e < V; ++e) s += v[i][e] * v[i][e];
+    for (int e = 0; e < 8; ++e) s += v[i][e] * v[i][e];
   }
   // the norm is that of the sum in 32 bits, not of its stored form: one rounding less on the way to y
   const float rs = 1.f / sqrtf(row_all<LPR, false>(s, sh) / (float)d + eps);
@@ -172,15 +222,15 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_fwd(const T* x, const T
   float top = 0.f;
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
-    const int j = (lane + LPR * i) * V;
+    const int j = (lane + LPR * i) * 8;
     if (j < d_live) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
+      for (int e = 0; e < 8; ++e) {
         v[i][e] = v[i][e] * rs * gr[i][e];
         const float a = fabsf(v[i][e]);
         top = a > top || a != a ? a : top;
       }
-      if (y) store_v<V>(y + base + j, v[i]);
+      if (y) store_n<ODD>(y + base + j, v[i], d - j);
     }
   }
   if (!y8) return;
@@ -191,18 +241,24 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_fwd(const T* x, const T
   if (lane == 0) y8_scale[row] = scale;
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
-    const int j = (lane + LPR * i) * V;
+    const int j = (lane + LPR * i) * 8;
     if (j < d) {
-      if constexpr (V == 8) {
-        int w[2];
+      int w[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(v[i][4 * h] * inv, v[i][4 * h + 1] * inv, 0, false);
-          w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(v[i][4 * h + 2] * inv, v[i][4 * h + 3] * inv, w[h], true);
-        }
+      for (int h = 0; h < 2; ++h) {
+        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(v[i][4 * h] * inv, v[i][4 * h + 1] * inv, 0, false);
+        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(v[i][4 * h + 2] * inv, v[i][4 * h + 3] * inv, w[h], true);
+      }
+      if (!ODD) {
         *reinterpret_cast<int2*>(y8 + base + j) = make_int2(w[0], w[1]);
+      } else if (d - j >= 8) {
+        typedef __attribute__((ext_vector_type(2))) int I2;
+        typedef I2 __attribute__((aligned(1))) Anywhere;
+        *reinterpret_cast<Anywhere*>(y8 + base + j) = I2{w[0], w[1]};
       } else {
-        y8[base + j] = to_e4m3(v[i][0] * inv);
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+          if (j + e < d) y8[base + j + e] = (unsigned char)(w[e / 4] >> 8 * (e % 4));
       }
     }
   }
@@ -210,46 +266,46 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_fwd(const T* x, const T
 
 // Blocks walk over the rows with a stride and keep the sums of dg of their columns in registers; partial[block][d].  A row stays in
 // registers as it was loaded, and where that is little enough the next one's loads are under way beside it.
-template <typename T, int LPR, int NCH, int V>
+template <typename T, int LPR, int NCH, bool ODD>
 __global__ void __launch_bounds__(threads_of(LPR), 4) k_rms_bwd(const T* dy, const T* r, const float* __restrict__ rstd,
                                                              const float* __restrict__ g, const T* add, T* dres, T* dx,
                                                              float* __restrict__ partial, int rows, int d, Drop dr) {
-  constexpr int RPB = threads_of(LPR) / LPR, REGS = V == 8 ? NCH * 2 * (int)sizeof(T) : NCH;
-  constexpr bool AHEAD = REGS <= (V == 8 ? 4 : 8);
+  constexpr int RPB = threads_of(LPR) / LPR, REGS = NCH * 2 * (int)sizeof(T);
+  constexpr bool AHEAD = REGS <= 4;
   __shared__ float sh[16];
-  __shared__ Numbers<LPR, V == 1 ? NCH : 0> numbers[RPB];
-  extern __shared__ float sums[];               // [RPB][LPR * NCH * V], where a block has several rows
+  __shared__ Numbers<ODD ? LPR : 0, ODD ? NCH : 0> numbers[RPB];
+  extern __shared__ float sums[];               // [RPB][LPR * NCH * 8], where a block has several rows
   const int lane = threadIdx.x % LPR, sub = threadIdx.x / LPR;
   auto& num = numbers[sub];
-  struct Row { Raw<T, V> r[NCH], y[NCH], a[NCH]; float rs; } now, next;
+  struct Row { Raw<T> r[NCH], y[NCH], a[NCH]; float rs; } now, next;
   auto fetch = [&](int row, Row& to) {
     const bool live = row < rows;               // rows share a wave: those past the end go along in its shuffles
     const size_t base = (size_t)row * d;
     to.rs = live ? rstd[row] : 0.f;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int j = (lane + LPR * i) * V;
+      const int j = (lane + LPR * i) * 8;
       to.r[i].zero();
       to.y[i].zero();
       to.a[i].zero();
       if (j < d && live) {
-        to.r[i].load(r + base + j);
-        to.y[i].load(dy + base + j);
-        if (add) to.a[i].load(add + base + j);
+        to.r[i].template load<ODD>(r + base + j, d - j);
+        to.y[i].template load<ODD>(dy + base + j, d - j);
+        if (add) to.a[i].template load<ODD>(add + base + j, d - j);
       }
     }
   };
   if (AHEAD) fetch(blockIdx.x * RPB + sub, next);
   const PhiloxKey key = philox_key(dr);
-  Raw<float, V> gg[NCH];
-  float pg[NCH][V];
+  Raw<float> gg[NCH];
+  float pg[NCH][8];
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
-    const int j = (lane + LPR * i) * V;
+    const int j = (lane + LPR * i) * 8;
     gg[i].zero();
-    if (j < d) gg[i].load(g + j);
+    if (j < d) gg[i].template load<ODD>(g + j, d - j);
 #pragma unroll
-    for (int e = 0; e < V; ++e) pg[i][e] = 0.f;
+    for (int e = 0; e < 8; ++e) pg[i][e] = 0.f;
   }
   for (int row0 = blockIdx.x * RPB; row0 < rows; row0 += gridDim.x * RPB) {
     const int row = row0 + sub;
@@ -266,7 +322,7 @@ __global__ void __launch_bounds__(threads_of(LPR), 4) k_rms_bwd(const T* dy, con
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
+      for (int e = 0; e < 8; ++e) {
         const float yx = now.y[i][e] * (now.r[i][e] * rs);
         pg[i][e] += yx;
         s += yx * gg[i][e];
@@ -274,26 +330,28 @@ __global__ void __launch_bounds__(threads_of(LPR), 4) k_rms_bwd(const T* dy, con
     s = row_all<LPR, false>(s, sh) / (float)d;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) { now.r[i].again(); now.y[i].again(); now.a[i].again(); }
-    if (V == 1 && dx && dr.thr) {
-      __syncthreads();                          // the row before has been read
-      draw_row(dr, key, base, d, num);
-      __syncthreads();
+    if constexpr (ODD) {
+      if (dx && dr.thr) {
+        __syncthreads();                        // the row before has been read
+        draw_row(dr, key, base, d, num);
+        __syncthreads();
+      }
     }
     if (!live) continue;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int j = (lane + LPR * i) * V;
+      const int j = (lane + LPR * i) * 8;
       if (j >= d) continue;
-      float o[V];
+      float o[8];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
+      for (int e = 0; e < 8; ++e) {
         o[e] = rs * (now.y[i][e] * gg[i][e] - now.r[i][e] * rs * s);
         if (add) o[e] += now.a[i][e];
       }
-      if (dres) store_v<V>(dres + base + j, o);
+      if (dres) store_n<ODD>(dres + base + j, o, d - j);
       if (dx) {
-        if (dr.thr) drop_v(dr, key, base, j, num, o);
-        store_v<V>(dx + base + j, o);
+        if (dr.thr) drop_row<ODD>(dr, key, base, j, num, o);
+        store_n<ODD>(dx + base + j, o, d - j);
       }
     }
   }
@@ -302,17 +360,18 @@ __global__ void __launch_bounds__(threads_of(LPR), 4) k_rms_bwd(const T* dy, con
   if constexpr (RPB == 1) {
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int j = (lane + LPR * i) * V;
+      const int j = (lane + LPR * i) * 8;
       if (j < d)
 #pragma unroll
-        for (int e = 0; e < V; ++e) out[j + e] = pg[i][e];
+        for (int e = 0; e < 8; ++e)
+          if (!ODD || j + e < d) out[j + e] = pg[i][e];
     }
   } else {
-    constexpr int W = LPR * NCH * V;
+    constexpr int W = LPR * NCH * 8;
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
 #pragma unroll
-      for (int e = 0; e < V; ++e) sums[sub * W + (lane + LPR * i) * V + e] = pg[i][e];
+      for (int e = 0; e < 8; ++e) sums[sub * W + (lane + LPR * i) * 8 + e] = pg[i][e];
     __syncthreads();
     for (int j = threadIdx.x; j < d; j += 256) {
       float t = 0.f;
@@ -355,28 +414,27 @@ __global__ void __launch_bounds__(1024) k_rms_sum(const float* __restrict__ part
   }
 }
 
-// Lanes and steps of a row: fn(integral constants LPR, NCH, V).
+// Lanes and steps of a row: fn(integral constants LPR, NCH, ODD).
 template <int N> using Int = std::integral_constant<int, N>;
 constexpr int kMaxWidth = 16384;
 bool shape_ok(int rows, int d) { return rows >= 0 && rows <= 1 << 30 && d >= 1 && d <= kMaxWidth && (size_t)rows * d <= (size_t)1 << 35; }
 template <typename F>
 hipError_t by_width(int d, bool vec, F&& fn) {
-  if (vec) {
-    if (d <= 64) return fn(Int<8>(), Int<1>(), Int<8>());
-    if (d <= 128) return fn(Int<16>(), Int<1>(), Int<8>());
-    if (d <= 256) return fn(Int<32>(), Int<1>(), Int<8>());
-    if (d <= 512) return fn(Int<64>(), Int<1>(), Int<8>());
-    if (d <= 1024) return fn(Int<64>(), Int<2>(), Int<8>());
-    if (d <= 2048) return fn(Int<256>(), Int<1>(), Int<8>());
-    if (d <= 4096) return fn(Int<256>(), Int<2>(), Int<8>());
-    if (d <= 8192) return fn(Int<1024>(), Int<1>(), Int<8>());
-    return fn(Int<1024>(), Int<2>(), Int<8>());
-  }
-  if (d <= 64) return fn(Int<64>(), Int<1>(), Int<1>());
-  if (d <= 512) return fn(Int<64>(), Int<8>(), Int<1>());
-  if (d <= 2048) return fn(Int<256>(), Int<8>(), Int<1>());
-  if (d <= 8192) return fn(Int<1024>(), Int<8>(), Int<1>());
-  return fn(Int<1024>(), Int<16>(), Int<1>());
+  // The rows' ends make the slowest wave of an odd row, and blocks of 1024 leave few others beside it (4000 rows of 8191, bf16, forward
+  // 47 us with blocks of 512, 73 with 1024).
+  auto go = [&](auto odd) {
+    constexpr bool ODD = decltype(odd)::value;
+    if (d <= 64) return fn(Int<8>(), Int<1>(), odd);
+    if (d <= 128) return fn(Int<16>(), Int<1>(), odd);
+    if (d <= 256) return fn(Int<32>(), Int<1>(), odd);
+    if (d <= 512) return fn(Int<64>(), Int<1>(), odd);
+    if (d <= 1024) return fn(Int<64>(), Int<2>(), odd);
+    if (d <= 2048) return fn(Int<256>(), Int<1>(), odd);
+    if (d <= 4096) return fn(Int<256>(), Int<2>(), odd);
+    if (d <= 8192) return fn(Int<ODD ? 512 : 1024>(), Int<ODD ? 2 : 1>(), odd);
+    return fn(Int<1024>(), Int<2>(), odd);
+  };
+  return vec ? go(std::false_type()) : go(std::true_type());
 }
 template <typename... P>
 bool aligned16(P... p) { return ((((uintptr_t)p) | ...) & 15) == 0; }
@@ -384,7 +442,7 @@ bool aligned16(P... p) { return ((((uintptr_t)p) | ...) & 15) == 0; }
 // Blocks of the backward kernel: as many as the chip holds at once (four waves a SIMD), each with several rows where there are more,
 // so that the partial sums stay small beside the tensors.
 int bwd_blocks(int rows, int rpb, int lpr) {
-  const int all = (rows + rpb - 1) / rpb, most = lpr > 256 ? 256 : 1024;
+  const int all = (rows + rpb - 1) / rpb, most = 262144 / (lpr > 256 ? lpr : 256);
   if (all <= most) return all;
   const int each = (all + most - 1) / most;      // the same number of rows for all
   return (all + each - 1) / each;
@@ -420,11 +478,12 @@ hipError_t op_rmsnorm_fwd(const OpCtx& c, const void* x, const void* res, const 
   const bool vec = d % 8 == 0 && aligned16(x, res, g, r, y) && ((uintptr_t)y8 & 7) == 0;
   auto go = [&](auto t) {
     typedef decltype(t) T;
-    return by_width(d, vec, [&](auto lpr, auto nch, auto v) {
-      constexpr int L = decltype(lpr)::value, N = decltype(nch)::value, V = decltype(v)::value, th = threads_of(L), rpb = th / L;
+    return by_width(d, vec, [&](auto lpr, auto nch, auto odd) {
+      constexpr int L = decltype(lpr)::value, N = decltype(nch)::value, th = threads_of(L), rpb = th / L;
+      constexpr bool ODD = decltype(odd)::value;
       constexpr int most = 1 << 21;              // a launch has less than 2^32 threads along x
       const int blocks = (rows + rpb - 1) / rpb;
-      k_rms_fwd<T, L, N, V><<<dim3(blocks < most ? blocks : most, (blocks + most - 1) / most), th, 0, c.stream>>>(
+      k_rms_fwd<T, L, N, ODD><<<dim3(blocks < most ? blocks : most, (blocks + most - 1) / most), th, 0, c.stream>>>(
           (const T*)x, (const T*)res, g, (T*)r, (T*)y, (unsigned char*)y8, y8_scale, rstd, rows, d, eps, dr);
       return hipGetLastError();
     });
@@ -442,10 +501,11 @@ hipError_t op_rmsnorm_bwd(const OpCtx& c, const void* dy, const void* r, const f
   const bool vec = d % 8 == 0 && aligned16(dy, r, g, add, dres, dx);
   auto go = [&](auto t) {
     typedef decltype(t) T;
-    return by_width(d, vec, [&](auto lpr, auto nch, auto v) {
-      constexpr int L = decltype(lpr)::value, N = decltype(nch)::value, V = decltype(v)::value, th = threads_of(L), rpb = th / L;
+    return by_width(d, vec, [&](auto lpr, auto nch, auto odd) {
+      constexpr int L = decltype(lpr)::value, N = decltype(nch)::value, th = threads_of(L), rpb = th / L;
+      constexpr bool ODD = decltype(odd)::value;
       const int blocks = bwd_blocks(rows, rpb, L);
-      k_rms_bwd<T, L, N, V><<<blocks, th, rpb > 1 ? rpb * L * N * V * 4 : 0, c.stream>>>(
+      k_rms_bwd<T, L, N, ODD><<<blocks, th, rpb > 1 ? rpb * L * N * 8 * 4 : 0, c.stream>>>(
           (const T*)dy, (const T*)r, rstd, g, (const T*)add, (T*)dres, (T*)dx, dg ? c.partial : nullptr, rows, d, dr);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess || !dg) return e;
