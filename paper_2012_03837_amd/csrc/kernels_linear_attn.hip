@@ -17,8 +17,7 @@
 // adds the chunk to it, and one with the chunk's own scores and their product with the values, which adds both parts of the output.
 // Wider heads, whose state fills the registers anyway: one wave does both.
 // Whatever has more bits than the compute dtype (scores times decay, values times decay, the state as an operand) is
-// split into two bf16 parts (three where the state itself is an output): the parts' products are exact and summed in fp32.  With one part
-// alone every such rounding adds an error as large as that of the rounded output.
+// split into three bf16 parts, which hold all its 24 bits: the parts' products are exact and summed in fp32.
 #include "common.h"
 #include "gemm_common.h"
 
@@ -27,6 +26,7 @@ namespace lp {
 namespace {
 
 constexpr int kChunk = 32;
+template <typename T> constexpr int kParts = sizeof(T) == 2 ? 3 : 1;       // operands that hold an fp32 value
 constexpr float kLog2e = 1.4426950408889634f;
 typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
@@ -76,22 +76,22 @@ __device__ __forceinline__ f32x8 frag_col(const float (*s)[LD], int r0, int c0, 
   for (int e = 0; e < 8; ++e) r[e] = s[r0 + 8 * (e / 4) + 4 * hf + e % 4][c0 + n];
   return r;
 }
-// fp32 values as NP operands whose sum they are (to 2^-9 NP); one where the compute dtype is fp32.  By twos: a conversion rounds a
-// pair, and the pair's rounded values are its two halves in place.
+// fp32 values as NP operands whose sum they are (three: all 24 bits); one where the compute dtype is fp32.  Each part is the upper half of what the
+// parts before it leave, so that a pair takes one byte permutation a part (8 x 1024 positions, 12 heads of 64, forward and backward: 97 us with parts
+// rounded by conversions, 91 so; with two parts, which leave 2^-17 of every such value, 81).
 template <int NP>
 __device__ __forceinline__ void split(const f32x8& v, bf16x8 (&f)[NP]) {
-  typedef __attribute__((ext_vector_type(2))) float f32x2;
   typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
   u32x4 w[NP];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    f32x2 r = {v[2 * e], v[2 * e + 1]};
+    float a = v[2 * e], b = v[2 * e + 1];
 #pragma unroll
     for (int s = 0; s < NP; ++s) {
-      const unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector(r, bf16x2));
-      w[s][e] = h;
-      r[0] -= __builtin_bit_cast(float, h << 16);
-      r[1] -= __builtin_bit_cast(float, h & 0xffff0000u);
+      const unsigned ia = __builtin_bit_cast(unsigned, a), ib = __builtin_bit_cast(unsigned, b);
+      w[s][e] = __builtin_amdgcn_perm(ib, ia, 0x07060302u);
+      a -= __builtin_bit_cast(float, ia & 0xffff0000u);
+      b -= __builtin_bit_cast(float, ib & 0xffff0000u);
     }
   }
 #pragma unroll
@@ -253,7 +253,7 @@ __device__ __forceinline__ const T* lowest(const T* p, int ld, bool back, int u0
 __device__ __forceinline__ int acc_row(int v, int hf) { return 8 * (v / 4) + 4 * hf + v % 4; }      // of an accumulator's value
 
 // state += sum over the chunk's positions of k (weight v)^T: all rows, columns 32 col ..
-template <typename T, int DK, int NP, int LD>
+template <typename T, int DK, int LD>
 __device__ __forceinline__ void add_outer(f32x16 (&state)[DK / 32], const T (*ks)[LD], const T (*vs)[LD], const float* weight, int col, int lane) {
   const int hf = lane >> 5;
 #pragma unroll
@@ -266,7 +266,7 @@ __device__ __forceinline__ void add_outer(f32x16 (&state)[DK / 32], const T (*ks
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[4 * x + e] = (float)v[4 * x + e] * t[e];
     }
-    typename Frag<T>::V f[NP];
+    typename Frag<T>::V f[kParts<T>];
     split(w, f);
 #pragma unroll
     for (int i = 0; i < DK / 32; ++i) state[i] = mma_parts(frag_col<LD>(ks, 16 * kk, 32 * i, lane), f, state[i]);
@@ -307,7 +307,7 @@ template <typename T, int DK> constexpr int kWavesPerSimd = DK <= 64 ? 3 : sizeo
 // that and lost more to the wider blocks (16 heads of 16384: 52 + 98 us became 57 + 106).
 template <typename T, int DK, bool VEC, bool FIN>
 __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k_linear_walk(LinearJobs jobs, LinearShape sh, int units) {
-  constexpr int ROLES = kRoles<DK>, NT = 2 * ROLES * DK, NP = sizeof(T) == 2 ? 2 : 1, NPS = sizeof(T) == 2 ? (FIN ? 3 : 2) : 1, ND = DK / 32;
+  constexpr int ROLES = kRoles<DK>, NT = 2 * ROLES * DK, NP = kParts<T>, ND = DK / 32;
   constexpr int LD = DK + kWalkPad<T, DK>;
   typedef typename Frag<T>::V FV;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k
   const float carry = power(at.g2, n + e0) * sh.scale, keep_whole = power(at.g2, kChunk);
   auto add = [&](const Tile<T, DK>& t, int c) {              // the chunk to the state
     scale(state, c == kChunk ? keep_whole : power(at.g2, c));
-    add_outer<T, DK, NPS, LD>(state, t.k, t.v, sm.weight[c < kChunk], col, lane);
+    add_outer<T, DK, LD>(state, t.k, t.v, sm.weight[c < kChunk], col, lane);
   };
   auto finish = [&]() {
     if (!FIN || !job.fin) return;
@@ -577,9 +577,9 @@ struct StateJobs { StateJob j[2]; };
 
 // Two waves for every 32 columns, which take a half of every 64 positions each; their sums are added at the end.  16 heads of 64, 16384
 // positions, bf16: 23.3 us for the 67 MB of k and v, 2.9 TB/s.
-template <typename T, int DK, bool VEC, bool FIN>
+template <typename T, int DK, bool VEC>
 __global__ void __launch_bounds__(4 * DK) k_linear_states(StateJobs jobs, LinearShape sh, int units) {
-  constexpr int NPS = sizeof(T) == 2 ? (FIN ? 3 : 2) : 1, ND = DK / 32, LD = DK + kPad<T>, R = 2 * kChunk;
+  constexpr int ND = DK / 32, LD = DK + kPad<T>, R = 2 * kChunk;
   struct Lds { __attribute__((aligned(16))) T k[2][R][LD], v[2][R][LD]; __attribute__((aligned(16))) float weight[2][R]; };
   extern __shared__ __attribute__((aligned(16))) char smem[];
   Lds& sm = *reinterpret_cast<Lds*>(smem);
@@ -632,7 +632,7 @@ __global__ void __launch_bounds__(4 * DK) k_linear_states(StateJobs jobs, Linear
     if (left > 0) fetch();
     __syncthreads();
     scale(state, c == R ? keep_whole : power(at.g2, c));
-    add_outer<T, DK, NPS, LD>(state, sm.k[slot] + kChunk * half, sm.v[slot] + kChunk * half, sm.weight[c < R] + kChunk * half, col, lane);
+    add_outer<T, DK, LD>(state, sm.k[slot] + kChunk * half, sm.v[slot] + kChunk * half, sm.weight[c < R] + kChunk * half, col, lane);
   }
   // the second halves' sums go through the tiles' memory
   float* part = reinterpret_cast<float*>(smem) + col * (ND * 16 * 64);
@@ -822,15 +822,11 @@ hipError_t states(const OpCtx& c, const StateJobs& jobs, int njobs, const Linear
   const hipError_t e = by_head(sh.dh, vec, [&](auto dk, auto v) {
     constexpr int DK = decltype(dk)::value, lds = state_lds<T, DK>();
     constexpr bool VEC = decltype(v)::value;
-    auto go = [&](auto f) {
-      constexpr bool FIN = decltype(f)::value;
-      static LdsLimit limit;
-      const hipError_t le = limit.raise(reinterpret_cast<const void*>(k_linear_states<T, DK, VEC, FIN>), lds);
-      if (le != hipSuccess) return le;
-      k_linear_states<T, DK, VEC, FIN><<<blocks, 4 * DK, lds, c.stream>>>(jobs, sh, units);
-      return hipGetLastError();
-    };
-    return jobs.j[0].fin || jobs.j[1].fin ? go(std::true_type()) : go(std::false_type());
+    static LdsLimit limit;
+    const hipError_t le = limit.raise(reinterpret_cast<const void*>(k_linear_states<T, DK, VEC>), lds);
+    if (le != hipSuccess) return le;
+    k_linear_states<T, DK, VEC><<<blocks, 4 * DK, lds, c.stream>>>(jobs, sh, units);
+    return hipGetLastError();
   });
   if (e != hipSuccess) return e;
   uintptr_t low = 0;

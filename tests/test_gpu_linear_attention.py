@@ -421,3 +421,70 @@ def test_gradients_against_differences(K, S, dh, lens):
         expect = float((grads[i] * step).sum())
         assert abs(moved - base - expect) <= off + off2 + 3e-6 * np.linalg.norm(grads[i]) * np.linalg.norm(step), "qkvs"[i]
         assert abs(expect) > 10 * (off + off2)              # the step is no smaller than what it is measured with
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("B,S,dh,lens", [(2, 300, 64, None), (1, 1200, 64, None), (2, 900, 64, [900, 411]), (1, 900, 32, None), (1, 900, 128, None), (2, 200, 96, None)])
+def test_outputs_do_not_depend_on_what_else_is_asked_for(K, dtype, B, S, dh, lens):
+    """o and dqkv are the same bits with and without s_out and ds0."""
+    import torch
+    case = Case(dtype, B, S, 2, dh, seed=11, lens=lens)
+    d = case.upload()
+    case.outputs()
+    case.forward(K)
+    case.backward(K)
+    both = d["o"].clone(), d["dqkv"].clone()
+    d["s_out"] = d["ds0"] = None
+    case.forward(K)
+    case.backward(K)
+    assert torch.equal(d["o"], both[0]) and torch.equal(d["dqkv"], both[1])
+
+
+def bf16_call(K, q, k, v, g, s0=None):
+    """One sequence and head of 64: o."""
+    import torch
+    qkv = torch.cat([torch.as_tensor(a, dtype=torch.float32) for a in (q, k, v)], 1).to("cuda", torch.bfloat16)
+    S = qkv.shape[0]
+    o = torch.empty(S, 64, device="cuda", dtype=torch.bfloat16)
+    n = K.lpk_linear_attention_scratch(1, S, 1, 64, 0)
+    K.lpk_linear_attention_fwd(1, qkv, torch.tensor([g], device="cuda"), None, None if s0 is None else torch.as_tensor(s0, dtype=torch.float32).cuda(), o, None,
+                               1, S, 1, 64, torch.empty(n, device="cuda") if n else None)
+    return o.float().cpu().numpy().astype(np.float64)
+
+
+@pytest.mark.parametrize("which", ["state", "score"])
+def test_bf16_operands_keep_32_bits_between_products(K, which):
+    """1 + 2^-8 + 2^-20 lies 2^-20 above the middle between two bf16 numbers and becomes the upper one; with 17 bits alone it is the middle, which goes to
+    the lower.  As an element of the state, and as a score (whose sum is exact in fp32)."""
+    x = 1 + 2.0 ** -8 + 2.0 ** -20
+    q, k, v = np.zeros((1, 64)), np.zeros((1, 64)), np.zeros((1, 64))
+    if which == "state":
+        s0 = np.zeros((1, 1, 64, 64))
+        s0[..., 3, :] = 8 * x
+        q[0, 3] = 1
+        o = bf16_call(K, q, k, v, 0.0, s0)
+    else:
+        q[0, :3] = 1, 2.0 ** -8, 2.0 ** -20
+        k[0, :3] = 1
+        v[:] = 8
+        o = bf16_call(K, q, k, v, 0.0)
+    assert (o == 1 + 2.0 ** -7).all()
+
+
+def test_bf16_values_keep_32_bits_under_their_decay(K):
+    """One key and value, then queries: o_t = l^t v / 8, one product and roundings of 2^-24: of the decay's exponent (up to 4 l^t's) and power, the weight, the value
+    times it, the scale, and two for each chunk between; an output is within half a step of its own 8 bits and those."""
+    S, g = 200, -0.013
+    rng = np.random.default_rng(12)
+    q, k, v = np.zeros((S, 64)), np.zeros((S, 64)), np.zeros((S, 64))
+    q[:, 5] = k[0, 5] = 1
+    v[0] = ops.bf16_round(rng.standard_normal(64).astype(np.float32))
+    worst = 0.0
+    for i in range(16):
+        gi = float(np.float32(g * (1 + i / 16)))
+        o = bf16_call(K, q, k, v, gi)
+        t = np.arange(S)[:, None]
+        exact = np.exp(gi * t) * v[0] / 8
+        half = np.exp2(np.floor(np.log2(np.abs(exact))) - 8)
+        worst = max(worst, float(((np.abs(o - exact) - half) / np.abs(exact) / (2.0 ** -24 * (10 + 2 * (t // 32)))).max()))
+    assert worst <= 1
