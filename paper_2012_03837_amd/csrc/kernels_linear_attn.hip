@@ -127,6 +127,22 @@ __device__ __forceinline__ void zero(f32x16& a) {
 }
 // l^n, n >= 0; l^0 is 1 also for a decay to nothing (log_decay = -inf, which comes in as a large finite number)
 __device__ __forceinline__ float power(float g2, int n) { return __builtin_amdgcn_exp2f(g2 * (float)n); }
+// l^n for a chain of products, one after another: rounded to 24 bits it would be off by the same share every time (4096 chunks of decays of
+// 1 - 2^-17: 1e-4 of the state), so that what rounding leaves out goes into the next factor, and the product of all is off by one unit.
+struct Chain {
+  float by, rest, off;
+  __device__ __forceinline__ Chain(float g2, int n) {
+    const float x = g2 * (float)n;
+    by = __builtin_amdgcn_exp2f(x);
+    rest = by < 0.5f ? 0.f : expm1f(x * 0.69314718056f) - (by - 1.f);      // lower ones leave nothing after some steps
+    off = 0.f;
+  }
+  __device__ __forceinline__ float next() {
+    const float t = off + rest, f = by + t;
+    off = t - (f - by);
+    return f;
+  }
+};
 __device__ __forceinline__ float decay_of(const float* log_decay, int h) {
   const float g = log_decay[h];
   return (g < -1e4f ? -1e4f : g) * kLog2e;
@@ -481,9 +497,10 @@ __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k
     }
     to += (ptrdiff_t)kChunk * dir * job.ldo;
   };
-  const float carry = power(at.g2, n + e0) * sh.scale, keep_whole = power(at.g2, kChunk);
+  const float carry = power(at.g2, n + e0) * sh.scale;
+  Chain whole(at.g2, kChunk);
   auto add = [&](const Tile<T, DK>& t, int c) {              // the chunk to the state
-    scale(state, c == kChunk ? keep_whole : power(at.g2, c));
+    scale(state, c == kChunk ? whole.next() : power(at.g2, c));
     add_outer<T, DK, LD>(state, t.k, t.v, sm.weight[c < kChunk], col, lane);
   };
   auto finish = [&]() {
@@ -624,14 +641,14 @@ __global__ void __launch_bounds__(4 * DK) k_linear_states(StateJobs jobs, Linear
     sm.weight[0][u] = power(at.g2, R - u - e0);
     sm.weight[1][u] = u < rest ? power(at.g2, rest - u - e0) : 0.f;
   }
-  const float keep_whole = power(at.g2, R);
+  Chain whole(at.g2, R);
   for (int u0 = first, slot = 0; u0 < stop; u0 += R, slot ^= 1) {
     const int c = stop - u0 < R ? stop - u0 : R;
     kr.store(sm.k[slot], dh);                                // read by nobody since the last barrier
     vr.store(sm.v[slot], dh);
     if (left > 0) fetch();
     __syncthreads();
-    scale(state, c == R ? keep_whole : power(at.g2, c));
+    scale(state, c == R ? whole.next() : power(at.g2, c));
     add_outer<T, DK, LD>(state, sm.k[slot] + kChunk * half, sm.v[slot] + kChunk * half, sm.weight[c < R] + kChunk * half, col, lane);
   }
   // the second halves' sums go through the tiles' memory
@@ -681,6 +698,7 @@ __global__ void __launch_bounds__(256) k_linear_scan(StateJobs jobs, LinearShape
   if (job.init) s = *reinterpret_cast<const FV*>(job.init + (size_t)bh * dd + x) * job.in_scale;
   const float g2 = decay_of(sh.log_decay, bh % sh.H);
   const int len = sh.length(bh / sh.H), span = sh.per * kChunk;
+  Chain whole(g2, span);
   for (int g = 0; g < sh.segments; g += U) {
     FV now[U];
 #pragma unroll
@@ -691,7 +709,7 @@ __global__ void __launch_bounds__(256) k_linear_scan(StateJobs jobs, LinearShape
       if (g + i >= sh.segments) break;
       *reinterpret_cast<FV*>(p + (size_t)(g + i) * dd) = s;
       const int left = len - (g + i) * span, c = left < 0 ? 0 : left < span ? left : span;
-      s = power(g2, c) * s + now[i];
+      s = (c == span ? whole.next() : power(g2, c)) * s + now[i];
     }
   }
   if (job.fin) *reinterpret_cast<FV*>(job.fin + (size_t)bh * dd + x) = s * job.out_scale;
@@ -711,7 +729,11 @@ __global__ void __launch_bounds__(256) k_linear_step(const T* __restrict__ qkv, 
     k[threadIdx.x] = to_f(row[H * dh + threadIdx.x]);
     v[threadIdx.x] = to_f(row[2 * H * dh + threadIdx.x]);
   }
-  const float l = power(decay_of(log_decay, h), 1);
+  // x l, near 1 as x + x (l - 1): l rounded itself would be off by the same share token after token
+  const float g2 = decay_of(log_decay, h);
+  const bool near = g2 > -1.f;
+  const float by = near ? expm1f(g2 * 0.69314718056f) : power(g2, 1);
+  auto next = [&](float x, float kv) { return __builtin_fmaf(x, by, near ? kv + x : kv); };
   float* s = state + (size_t)bh * dh * dh;
   __syncthreads();
   const int per = (dh + 3) / 4, rows = 256 / per, c = threadIdx.x % per * 4, r0 = threadIdx.x / per;     // threads of a row
@@ -730,7 +752,7 @@ __global__ void __launch_bounds__(256) k_linear_step(const T* __restrict__ qkv, 
           if (rr < dh) {
             const float kr = k[rr], qr = q[rr];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { x[i][e] = l * x[i][e] + kr * v[c + e]; acc[e] += qr * x[i][e]; }
+            for (int e = 0; e < 4; ++e) { x[i][e] = next(x[i][e], kr * v[c + e]); acc[e] += qr * x[i][e]; }
             *reinterpret_cast<f32x4*>(s + (size_t)rr * dh + c) = x[i];
           }
         }
@@ -740,7 +762,7 @@ __global__ void __launch_bounds__(256) k_linear_step(const T* __restrict__ qkv, 
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (c + e < dh) {
-            const float x = l * s[(size_t)r * dh + c + e] + k[r] * v[c + e];
+            const float x = next(s[(size_t)r * dh + c + e], k[r] * v[c + e]);
             s[(size_t)r * dh + c + e] = x;
             acc[e] += q[r] * x;
           }

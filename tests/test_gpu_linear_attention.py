@@ -488,3 +488,55 @@ def test_bf16_values_keep_32_bits_under_their_decay(K):
         half = np.exp2(np.floor(np.log2(np.abs(exact))) - 8)
         worst = max(worst, float(((np.abs(o - exact) - half) / np.abs(exact) / (2.0 ** -24 * (10 + 2 * (t // 32)))).max()))
     assert worst <= 1
+
+
+def decayed(g, n):
+    """l^n in 64 bits, and how far c roundings of the state may be from it: each is off by half a unit at most and independent of the others (a step takes away 2^-12 of
+    the state or more, and the next step's by a unit less), so that their sum has a spread of 2^-24 sqrt(c / 3), of which five; the exponent has a rounding or
+    two (its share of n g each), a power as well."""
+    g = g.astype(np.float64)
+    return lambda c: (np.exp(n * g), 2.0 ** -24 * (5 * np.sqrt(c / 3) + 4 * np.abs(n * g) + 8))
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("S,H,dh", [(131072, 257, 1), (131072, 2, 8)])
+def test_a_state_decays_by_the_power_however_long_the_chain(K, dtype, S, H, dh):
+    """Keys, values, queries and dout of zeros: s_out = l^S s0 and ds0 = l^S ds_out after 4096 chunks, one after another (many heads) or in segments."""
+    import torch
+    n = [K.lpk_linear_attention_scratch(1, S, H, dh, b) for b in (0, 1)]
+    assert (max(n) == 0) == (H == 257)
+    g = np.log1p(-np.exp2(-np.linspace(12, 17, H))).astype(np.float32)
+    tdt = torch.bfloat16 if dtype else torch.float32
+    qkv, dqkv = torch.zeros(S, 3 * H * dh, device="cuda", dtype=tdt), torch.ones(S, 3 * H * dh, device="cuda", dtype=tdt)
+    o, dout = torch.ones(S, H * dh, device="cuda", dtype=tdt), torch.zeros(S, H * dh, device="cuda", dtype=tdt)
+    s0 = 1 + torch.rand(1, H, dh, dh, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    s_out, ds0 = torch.empty_like(s0), torch.empty_like(s0)
+    decay, ws = torch.from_numpy(g).cuda(), torch.empty(max(n) + 1, device="cuda")
+    K.lpk_linear_attention_fwd(dtype, qkv, decay, None, s0, o, s_out, 1, S, H, dh, ws)
+    # o_t = l^{t + 1} q_t s0 with q_t = 0; dq_t = 0 likewise
+    K.lpk_linear_attention_bwd(dtype, qkv, decay, None, s0, dout, s0, dqkv, ds0, 1, S, H, dh, ws)
+    want, tol = decayed(g, S)(S / 32)
+    for got in (s_out, ds0):
+        ratio = (got.double() / s0.double()).cpu().numpy().reshape(H, -1)
+        assert (np.abs(ratio / want[:, None] - 1) <= tol[:, None]).all()
+    assert not o.any() and not dqkv.any()
+
+
+def test_a_state_decays_by_the_power_token_after_token(K):
+    """8192 roundings, as above, but not independent at every decay: with m = 1 - l a step takes m s units away, the next one m^2 s 2^24 units less, that difference
+    falls by m^3 s 2^24 = 0.94 units a step at m = 0.0038222, and near a whole number the same roundings come again and again (the recurrence rounded exactly, on the
+    host: 2.75e-5 there, whatever the state begins with, and 2.0e-6 to 3.0e-6 as the root mean square over these decays; with l rounded instead 1.5e-4).
+    So the root mean square over the decays counts, of which the spread above is one part: twice that is allowed; and n halves of a unit for each, which is all that
+    can come together."""
+    import torch
+    H, n = 256, 8192
+    g = np.log1p(-np.exp2(-np.linspace(8, 12, H))).astype(np.float32)
+    decay = torch.from_numpy(g).cuda()
+    s0 = 1 + torch.rand(1, H, 1, 1, device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+    state, qkv, o = s0.clone(), torch.zeros(1, 3 * H, device="cuda"), torch.empty(1, H, device="cuda")
+    for _ in range(n):
+        K.lpk_linear_attention_step(0, qkv, decay, state, o, 1, H, 1)
+    want, tol = decayed(g, n)(n)
+    off = np.abs((state.double() / s0.double()).cpu().numpy().reshape(H) / want - 1)
+    assert np.sqrt((off ** 2).mean()) <= 2.0 ** -24 * (2 * np.sqrt(n / 3) + 4 * np.abs(n * g.astype(np.float64)).mean() + 8)
+    assert (off <= tol + n * 2.0 ** -24).all()
