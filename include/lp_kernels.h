@@ -125,7 +125,8 @@ int lpk_dropout(int dtype, const void* x, const void* res, void* y, size_t n, fl
  * res may be null; p, rng_dev and site as in lpk_dropout (index: row * d + column; p 0: nothing is dropped).  r (may be null, may be x
  * or res) and y (compute dtype, may be null) are outputs, rstd (fp32 [rows], may be null) is kept for the backward call; the norm is
  * taken of the sum before its rounding to the compute dtype.  y8 (may be null) receives y in 8 bits, e4m3, with one scale for
- * a row: y8 = y / y8_scale[row], y8_scale = max |y| / 448 (1 for a row of zeros).  At least one of y and y8 is wanted.
+ * a row: y8 = y / y8_scale[row], the fp32 quotient, y8_scale = max |y| / 448 (1 for a row of zeros, otherwise 2^-126 at least).  At least one
+ * of y and y8 is wanted.
  * Backward, of r as stored (x itself where there was neither res nor dropout): dres = gradient of r (+ add, the stream's own, may be
  * null), dx = that of x where p > 0 (null where it is not wanted: with p 0 it is dres), dg (+)= sum over rows (may be null).  dres and
  * dx may be dy, r or add.  scratch_dev: lpk_rmsnorm_scratch floats where dg is wanted (needs no device). */

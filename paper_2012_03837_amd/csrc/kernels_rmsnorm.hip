@@ -237,6 +237,13 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_fwd(const T* x, const T
   top = row_all<LPR, true>(top, sh);
   // a row so small that 1 / s would overflow takes the smallest normal number
   const float least = 1.17549435e-38f, scale = top == 0.f ? 1.f : top / 448.f < least ? least : top / 448.f, inv = 1.f / scale;
+  // the quotient as rounded once: a product with the rounded 1 / s, one unit off here and there, would move values next to the middle between
+  // two 8-bit ones.  Its remainder corrects it; behind an infinite scale all that is finite is 0.
+  const float back = scale < INFINITY ? scale : 0.f;
+  auto quotient = [&](float a) {
+    const float q = a * inv;
+    return __builtin_fmaf(__builtin_fmaf(-q, back, a), inv, q);
+  };
   if (!live) return;
   if (lane == 0) y8_scale[row] = scale;
 #pragma unroll
@@ -246,8 +253,8 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_fwd(const T* x, const T
       int w[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(v[i][4 * h] * inv, v[i][4 * h + 1] * inv, 0, false);
-        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(v[i][4 * h + 2] * inv, v[i][4 * h + 3] * inv, w[h], true);
+        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(v[i][4 * h]), quotient(v[i][4 * h + 1]), 0, false);
+        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(v[i][4 * h + 2]), quotient(v[i][4 * h + 3]), w[h], true);
       }
       if (!ODD) {
         *reinterpret_cast<int2*>(y8 + base + j) = make_int2(w[0], w[1]);

@@ -450,3 +450,48 @@ def test_norm_of_very_many_rows(K):
     # five operations in fp32, each off by half a unit
     assert bool((y[:rows].double() - 2 * x.double() / (x.double() ** 2 + 1e-5).sqrt()).abs().max() <= 5 * 2.0 ** -24 * 2)
     assert bool((y[rows:] == 7).all())
+
+
+def values_beside_middles(scale):
+    """Gains whose quotients by `scale` lie at the middles between two 8-bit numbers and one unit beside them, the largest 448 scale."""
+    step = [m * 2.0 ** e / 8 for e in range(-6, 9) for m in range(8, 16)]
+    step = [v for v in step if v <= 448]
+    mid = np.array([(a + b) / 2 for a, b in zip(step, step[1:])])
+    at = (mid * float(scale)).astype(np.float32)
+    g = np.concatenate([at, np.nextafter(at, np.float32(0)), np.nextafter(at, np.float32(np.inf))])
+    return np.concatenate([g, np.resize(g[::-1], 512 - 1 - g.size), [np.float32(448 * float(scale))]]).astype(np.float32)
+
+
+@pytest.mark.parametrize("odd", [0, 1])
+def test_8_bit_values_are_quotients_rounded_once(K, odd):
+    """Rows of 1 and -1 without eps: y = g x exactly, and y8 = e4m3(y / s) with the quotient in fp32."""
+    import torch
+    rng = np.random.default_rng(9)
+    told = 0
+    for _ in range(20):
+        g = values_beside_middles(np.float32(2.0 ** rng.uniform(-3, 3)))[odd:]
+        d = g.size
+        x = rng.choice(np.array([-1, 1], np.float32), (2, d))
+        b = Bench(0, d)
+        y, y8, s8 = b.room((2, d)), b.room((2, d), torch.float8_e4m3fn), b.room((2,))
+        K.lpk_rmsnorm_fwd(0, b.dev(x), None, b.dev(g), None, y, y8, s8, None, 2, d, 0.0)
+        assert np.array_equal(y.cpu().numpy(), g * x)
+        scale = np.float32(g.max()) / np.float32(448)
+        assert (s8.cpu().numpy() == scale).all()
+        e4m3 = lambda a: torch.from_numpy(a.astype(np.float32)).to(torch.float8_e4m3fn).float().numpy()  # noqa: E731
+        want = e4m3(g / scale)
+        assert np.array_equal(y8.float().cpu().numpy(), want * x)
+        told += int((e4m3(g * (np.float32(1) / scale)) != want).sum())
+    assert told > 20                    # values that a product with 1 / s would have moved
+
+
+def test_8_bit_rows_with_an_infinity(K):
+    """A gain of infinity: its column is NaN, the rest of the row, over an infinite scale, zeros."""
+    import torch
+    b = Bench(0, 3)
+    g = np.ones(64, np.float32)
+    g[7] = np.inf
+    y8, s8 = b.room((1, 64), torch.float8_e4m3fn), b.room((1,))
+    K.lpk_rmsnorm_fwd(0, b.dev(np.ones((1, 64), np.float32)), None, b.dev(g), None, None, y8, s8, None, 1, 64, 1e-5)
+    got = host(y8)[0]
+    assert np.isnan(got[7]) and not np.delete(got, 7).any() and np.isinf(host(s8)[0])
