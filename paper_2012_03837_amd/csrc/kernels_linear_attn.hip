@@ -791,8 +791,8 @@ constexpr int kMaxHead = 128;
 struct Cut { int segments, per; };
 Cut cut_of(int dt, int B, int S, int H, int dh, int jobs) {
   const int chunks = (S + kChunk - 1) / kChunk, alone = dt == F32 && dh > 96;
-  const long blocks = (long)B * H * jobs, once = 256 * (dh <= 64 ? 3 : alone ? 1 : 2);
-  long want = blocks > 0 ? once / blocks : 1;
+  const long blocks = B > 0 ? (long)B * H * jobs : 1, once = 256 * (dh <= 64 ? 3 : alone ? 1 : 2);
+  long want = once / blocks;
   if (alone && want < 3) want = 2 * once / blocks;
   const long most = chunks / 4;
   if (want > most) want = most;

@@ -97,3 +97,15 @@ def test_wrappers_refuse_what_the_kernels_would_misread(K):
     x = torch.zeros(64, device="cuda")
     with pytest.raises(K.KernelError):
         K.lpk_dropout(0, x, None, x, 0.5, torch.zeros(2, device="cuda", dtype=torch.int32), 0)
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+@pytest.mark.parametrize("dh", [1, 64, 96, 97, 128])
+def test_workspace_of_an_empty_batch(dh, backward):
+    """In a process of its own: a division by zero ends it."""
+    import os
+    import subprocess
+    import sys
+    code = f"from paper_2012_03837_amd import kernels as K; print([K.lpk_linear_attention_scratch(0, S, 4, {dh}, {backward}) for S in (0, 1, 4096)])"
+    run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert run.returncode == 0 and run.stdout.split() == ["[0,", "0,", "0]"], run
