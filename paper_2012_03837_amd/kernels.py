@@ -117,38 +117,45 @@ def _fn(name):
     return f
 
 
-def _at(t, size=4):
-    """Address of a tensor (None: none) whose elements have `size` bytes (0: whatever they have, nothing reads them)."""
+_T = {}          # element types by the dtype argument, and of the lengths, the 8-bit values and the generator's numbers
+
+
+def _real(dtype):
+    """Types of the operands of a dtype argument; a call's first one fills the table."""
+    if not _T:
+        import torch
+        _T.update({0: (torch.float32,), 1: (torch.bfloat16,), "i32": (torch.int32,), "u64": (torch.int64, torch.uint64),
+                   "e4m3": (torch.float8_e4m3fn, torch.uint8), "torch": torch})
+    if dtype in (0, 1):
+        return _T[dtype]
+    raise KernelError(f"dtype {dtype!r}: 0 (fp32) or 1 (bf16) is needed")
+
+
+def _at(t, types, n, dev):
+    """Address of a tensor (None: none) of one of the types (None: nothing reads it) with n elements at least, on the device of that number."""
     if t is None:
         return None
-    if t.is_contiguous() and (t.itemsize == size or not size) and t.is_cuda:
+    if (types is None or t.dtype in types) and t.numel() >= n and t.is_contiguous() and t.get_device() == dev:
         return t.data_ptr()
-    raise KernelError(f"{t.dtype} tensor of {tuple(t.shape)}, strides {t.stride()} on {t.device}: a contiguous one of {size}-byte elements on the "
-                      "device is needed")
+    raise KernelError(f"{t.dtype} tensor of {tuple(t.shape)}, strides {t.stride()} on {t.device}: at least {n} contiguous elements of "
+                      f"{'any type' if types is None else ' or '.join(map(str, types))} on the first tensor's device are needed")
 
 
-def _bytes(dtype):
-    return 2 if dtype == 1 else 4
+def _none(name):
+    raise KernelError(f"{name}: no tensor")
 
 
-_torch = None
-
-
-def _run(name, where, *args):
-    """Calls entry point `name`, its last argument the current stream of the device that tensor `where` is on."""
-    global _torch
-    if _torch is None:
-        import torch
-        _torch = torch
-    dev = where.get_device()
+def _run(name, dev, *args):
+    """Calls entry point `name`, its last argument the current stream of device number dev."""
     if dev < 0:
-        raise KernelError(f"{name}: tensors on {where.device}")
+        raise KernelError(f"{name}: tensors on the host")
+    torch = _T["torch"]
     # the device's number and the stream's handle without the objects around them: 0.2 us instead of 3.3, of 6 for a call
-    rt = _torch._C
+    rt = torch._C
     if dev == rt._cuda_getDevice():
         rc = (_entry.get(name) or _fn(name))(*args, rt._cuda_getCurrentRawStream(dev))
     else:
-        with _torch.cuda.device(dev):
+        with torch.cuda.device(dev):
             rc = _fn(name)(*args, rt._cuda_getCurrentRawStream(dev))
     if rc:
         _ck(rc, name)
@@ -164,26 +171,39 @@ def lpk_linear_attention_scratch(B, S, H, dh, backward):
 
 
 def lpk_linear_attention_fwd(dtype, qkv, log_decay, lens, s0, o, s_out, B, S, H, dh, scratch=None):
-    e = _bytes(dtype) if S else 0
-    _run("lpk_linear_attention_fwd", qkv, dtype, _at(qkv, e), _at(log_decay), _at(lens), _at(s0), _at(o, e), _at(s_out), B, S, H, dh,
-         _at(scratch), _size(scratch))
+    e, dev = _T.get(dtype) or _real(dtype), _none("lpk_linear_attention_fwd") if qkv is None else qkv.get_device()
+    e = e if S else None
+    f, n, state = _T[0], B * S * H * dh, B * H * dh * dh
+    _run("lpk_linear_attention_fwd", dev, dtype, _at(qkv, e, 3 * n, dev), _at(log_decay, f, H, dev), _at(lens, _T["i32"], B, dev),
+         _at(s0, f, state, dev), _at(o, e, n, dev), _at(s_out, f, state, dev), B, S, H, dh, _at(scratch, f, 0, dev), _size(scratch))
 
 
 def lpk_linear_attention_bwd(dtype, qkv, log_decay, lens, s0, dout, ds_out, dqkv, ds0, B, S, H, dh, scratch=None):
-    e = _bytes(dtype) if S else 0
-    _run("lpk_linear_attention_bwd", qkv, dtype, _at(qkv, e), _at(log_decay), _at(lens), _at(s0), _at(dout, e), _at(ds_out), _at(dqkv, e),
-         _at(ds0), B, S, H, dh, _at(scratch), _size(scratch))
+    e, dev = _T.get(dtype) or _real(dtype), _none("lpk_linear_attention_bwd") if qkv is None else qkv.get_device()
+    e = e if S else None
+    f, n, state = _T[0], B * S * H * dh, B * H * dh * dh
+    _run("lpk_linear_attention_bwd", dev, dtype, _at(qkv, e, 3 * n, dev), _at(log_decay, f, H, dev), _at(lens, _T["i32"], B, dev),
+         _at(s0, f, state, dev), _at(dout, e, n, dev), _at(ds_out, f, state, dev), _at(dqkv, e, 3 * n, dev), _at(ds0, f, state, dev), B, S, H, dh,
+         _at(scratch, f, 0, dev), _size(scratch))
 
 
 def lpk_linear_attention_step(dtype, qkv, log_decay, state, o, B, H, dh):
-    e = _bytes(dtype)
-    _run("lpk_linear_attention_step", qkv, dtype, _at(qkv, e), _at(log_decay), _at(state), _at(o, e), B, H, dh)
+    e, dev, n = _T.get(dtype) or _real(dtype), _none("lpk_linear_attention_step") if qkv is None else qkv.get_device(), B * H * dh
+    f = _T[0]
+    _run("lpk_linear_attention_step", dev, dtype, _at(qkv, e, 3 * n, dev), _at(log_decay, f, H, dev), _at(state, f, n * dh, dev), _at(o, e, n, dev),
+         B, H, dh)
+
+
+def _site(site):
+    raise KernelError(f"site {site}: a number of 32 bits is needed")
 
 
 def lpk_dropout(dtype, x, res, y, p, rng, site):
     """rng: two 64-bit integers (seed, step) on the device."""
-    e = _bytes(dtype)
-    _run("lpk_dropout", x, dtype, _at(x, e), _at(res, e), _at(y, e), x.numel(), p, _at(rng, 8), site)
+    e, dev = _T.get(dtype) or _real(dtype), _none("lpk_dropout") if x is None else x.get_device()
+    n = x.numel()
+    _run("lpk_dropout", dev, dtype, _at(x, e, n, dev), _at(res, e, n, dev), _at(y, e, n, dev), n, p, _at(rng, _T["u64"], 2, dev),
+         site if -1 < site < 1 << 32 else _site(site))
 
 
 def lpk_rmsnorm_scratch(rows, d):
@@ -192,15 +212,19 @@ def lpk_rmsnorm_scratch(rows, d):
 
 
 def lpk_rmsnorm_fwd(dtype, x, res, g, r, y, y8, y8_scale, rstd, rows, d, eps, p=0.0, rng=None, site=0):
-    e = _bytes(dtype)
-    _run("lpk_rmsnorm_fwd", x, dtype, _at(x, e), _at(res, e), _at(g), _at(r, e), _at(y, e), _at(y8, 1), _at(y8_scale), _at(rstd), rows, d, eps, p,
-         _at(rng, 8), site)
+    e, dev, n = _T.get(dtype) or _real(dtype), _none("lpk_rmsnorm_fwd") if x is None else x.get_device(), rows * d
+    f = _T[0]
+    _run("lpk_rmsnorm_fwd", dev, dtype, _at(x, e, n, dev), _at(res, e, n, dev), _at(g, f, d, dev), _at(r, e, n, dev), _at(y, e, n, dev),
+         _at(y8, _T["e4m3"], n, dev), _at(y8_scale, f, rows, dev), _at(rstd, f, rows, dev), rows, d, eps, p, _at(rng, _T["u64"], 2, dev),
+         site if -1 < site < 1 << 32 else _site(site))
 
 
 def lpk_rmsnorm_bwd(dtype, dy, r, rstd, g, add, dres, dx, dg, rows, d, accumulate=0, scratch=None, p=0.0, rng=None, site=0):
-    e = _bytes(dtype)
-    _run("lpk_rmsnorm_bwd", dy, dtype, _at(dy, e), _at(r, e), _at(rstd), _at(g), _at(add, e), _at(dres, e), _at(dx, e), _at(dg), rows, d, accumulate,
-         p, _at(rng, 8), site, _at(scratch), _size(scratch))
+    e, dev, n = _T.get(dtype) or _real(dtype), _none("lpk_rmsnorm_bwd") if dy is None else dy.get_device(), rows * d
+    f = _T[0]
+    _run("lpk_rmsnorm_bwd", dev, dtype, _at(dy, e, n, dev), _at(r, e, n, dev), _at(rstd, f, rows, dev), _at(g, f, d, dev), _at(add, e, n, dev),
+         _at(dres, e, n, dev), _at(dx, e, n, dev), _at(dg, f, d, dev), rows, d, accumulate, p, _at(rng, _T["u64"], 2, dev),
+         site if -1 < site < 1 << 32 else _site(site), _at(scratch, f, 0, dev), _size(scratch))
 
 
 def lpk_layernorm_fwd(dtype, x, g, b, y, mean, rstd, rows, d):

@@ -109,3 +109,77 @@ def test_workspace_of_an_empty_batch(dh, backward):
     code = f"from paper_2012_03837_amd import kernels as K; print([K.lpk_linear_attention_scratch(0, S, 4, {dh}, {backward}) for S in (0, 1, 4096)])"
     run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert run.returncode == 0 and run.stdout.split() == ["[0,", "0,", "0]"], run
+
+
+# ------------------------------------------------------------------------------------------------ the wrappers' own checks
+# Tensors of the host: what is right but for that is refused for it last, everything else by its own check before.
+def tensors(sizes):
+    import torch
+    types = dict(e=torch.bfloat16, f=torch.float32, i=torch.int32, u=torch.int64, q=torch.float8_e4m3fn)
+    return {n: torch.zeros(size, dtype=types[t]) if t else size for n, (t, size) in sizes.items()}
+
+
+B_, S_, H_, D_, R_ = 2, 10, 3, 16, 5
+N_, STATE_ = B_ * S_ * H_ * D_, B_ * H_ * D_ * D_
+GEOMETRY = dict(B=(None, B_), S=(None, S_), H=(None, H_), dh=(None, D_))
+WRAPPED = {
+    "lpk_linear_attention_fwd": dict(dtype=(None, 1), qkv=("e", 3 * N_), log_decay=("f", H_), lens=("i", B_), s0=("f", STATE_), o=("e", N_), s_out=("f", STATE_),
+                                     **GEOMETRY, scratch=("f", 7)),
+    "lpk_linear_attention_bwd": dict(dtype=(None, 1), qkv=("e", 3 * N_), log_decay=("f", H_), lens=("i", B_), s0=("f", STATE_), dout=("e", N_), ds_out=("f", STATE_),
+                                     dqkv=("e", 3 * N_), ds0=("f", STATE_), **GEOMETRY, scratch=("f", 7)),
+    "lpk_linear_attention_step": dict(dtype=(None, 1), qkv=("e", 3 * B_ * H_ * D_), log_decay=("f", H_), state=("f", STATE_), o=("e", B_ * H_ * D_), B=(None, B_),
+                                      H=(None, H_), dh=(None, D_)),
+    "lpk_dropout": dict(dtype=(None, 1), x=("e", 100), res=("e", 100), y=("e", 100), p=(None, 0.1), rng=("u", 2), site=(None, 0)),
+    "lpk_rmsnorm_fwd": dict(dtype=(None, 1), x=("e", R_ * D_), res=("e", R_ * D_), g=("f", D_), r=("e", R_ * D_), y=("e", R_ * D_), y8=("q", R_ * D_),
+                            y8_scale=("f", R_), rstd=("f", R_), rows=(None, R_), d=(None, D_), eps=(None, 1e-5), p=(None, 0.1), rng=("u", 2), site=(None, 0)),
+    "lpk_rmsnorm_bwd": dict(dtype=(None, 1), dy=("e", R_ * D_), r=("e", R_ * D_), rstd=("f", R_), g=("f", D_), add=("e", R_ * D_), dres=("e", R_ * D_),
+                            dx=("e", R_ * D_), dg=("f", D_), rows=(None, R_), d=(None, D_), accumulate=(None, 0), scratch=("f", R_ * D_), p=(None, 0.1), rng=("u", 2),
+                            site=(None, 0)),
+}
+OPERANDS = [(n, a) for n, args in WRAPPED.items() for a, (t, _) in args.items() if t]
+
+
+@pytest.mark.parametrize("name", WRAPPED)
+def test_wrappers_reach_the_device_check(K, name):
+    args = tensors(WRAPPED[name])
+    with pytest.raises(K.KernelError, match="tensors on the host"):
+        getattr(K, name)(*args.values())
+    with pytest.raises(K.KernelError, match="dtype 2"):
+        getattr(K, name)(*(args | dict(dtype=2)).values())
+
+
+@pytest.mark.parametrize("name,arg", OPERANDS)
+def test_wrappers_refuse_tensors_of_another_type(K, name, arg):
+    """Also of the same width: lengths as floats, halves for bf16, doubles for the generator's numbers."""
+    import torch
+    args = tensors(WRAPPED[name])
+    other = {1: torch.int8, 2: torch.float16, 4: torch.float32 if args[arg].dtype == torch.int32 else torch.int32, 8: torch.float64}[args[arg].itemsize]
+    for dt in (other, torch.float64):
+        with pytest.raises(K.KernelError, match="elements of"):
+            getattr(K, name)(*(args | {arg: args[arg].to(dt)}).values())
+
+
+@pytest.mark.parametrize("name,arg", [x for x in OPERANDS if x[1] not in ("scratch",) and x != ("lpk_dropout", "x")])
+def test_wrappers_refuse_tensors_that_are_too_small(K, name, arg):
+    import torch
+    args = tensors(WRAPPED[name])
+    with pytest.raises(K.KernelError, match=f"at least {args[arg].numel()} contiguous"):
+        getattr(K, name)(*(args | {arg: args[arg][:-1]}).values())
+    with pytest.raises(K.KernelError, match="tensors on the host"):             # larger ones, and in two dimensions, are taken
+        getattr(K, name)(*(args | {arg: torch.cat([args[arg], args[arg]]).view(2, -1)}).values())
+    with pytest.raises(K.KernelError, match="contiguous"):
+        getattr(K, name)(*(args | {arg: torch.cat([args[arg], args[arg]])[::2]}).values())
+
+
+def test_wrappers_refuse_numbers_that_would_wrap(K):
+    for name in ("lpk_dropout", "lpk_rmsnorm_fwd", "lpk_rmsnorm_bwd"):
+        for site in (-1, 1 << 32):
+            with pytest.raises(K.KernelError, match="site"):
+                getattr(K, name)(*(tensors(WRAPPED[name]) | dict(site=site)).values())
+    for name, arg in (("lpk_linear_attention_fwd", "S"), ("lpk_linear_attention_bwd", "B"), ("lpk_linear_attention_step", "H"), ("lpk_rmsnorm_fwd", "rows"),
+                      ("lpk_rmsnorm_bwd", "d")):
+        args = tensors(WRAPPED[name])
+        with pytest.raises(K.KernelError, match="at least"):
+            getattr(K, name)(*(args | {arg: args[arg] + (1 << 32)}).values())
+    with pytest.raises(K.KernelError, match="no tensor"):
+        K.lpk_dropout(0, None, None, None, 0.0, None, 0)
