@@ -540,3 +540,67 @@ def test_a_state_decays_by_the_power_token_after_token(K):
     off = np.abs((state.double() / s0.double()).cpu().numpy().reshape(H) / want - 1)
     assert np.sqrt((off ** 2).mean()) <= 2.0 ** -24 * (2 * np.sqrt(n / 3) + 4 * np.abs(n * g.astype(np.float64)).mean() + 8)
     assert (off <= tol + n * 2.0 ** -24).all()
+
+
+# ------------------------------------------------------------------------------------------------ long axes, whatever the sizes
+def cut_case(K, dtype, B, S, H, dh, **kw):
+    """A case both directions of which are cut into segments."""
+    assert all(K.lpk_linear_attention_scratch(B, S, H, dh, b) > 0 for b in (0, 1))
+    return Case(dtype, B, S, H, dh, **kw)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("dh", [1, 3, 8, 20, 33, 40, 72, 96, 100, 127])
+def test_segments_of_all_head_sizes(K, dtype, dh):
+    cut_case(K, dtype, 2, 640, 2, dh, seed=dh).check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("dh", [32, 64, 96, 128, 63])
+@pytest.mark.parametrize("lens", [None, [640, 317]])
+def test_segments_without_states(K, dtype, dh, lens):
+    cut_case(K, dtype, 2, 640, 2, dh, seed=dh, states=False, lens=lens).check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("dh,states", [(64, True), (64, False), (96, True), (128, True), (21, True)])
+def test_segments_of_unaligned_buffers(K, dtype, dh, states):
+    cut_case(K, dtype, 2, 650, 2, dh, seed=6, states=states, shift=1).check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("decay", [[0.0, 0.0], [-np.inf, -50.0], [-1e-4, -4.0]])
+@pytest.mark.parametrize("lens", [None, [0, 641]])
+def test_segments_of_decays_at_their_limits(K, dtype, decay, lens):
+    cut_case(K, dtype, 2, 700, 2, 64, seed=5, decay=decay, lens=lens).check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("states", [False, True])
+def test_heads_of_96_uncut(K, dtype, states):
+    assert K.lpk_linear_attention_scratch(2, 150, 2, 96, 1) == 0
+    Case(dtype, 2, 150, 2, 96, seed=1, states=states).check(K)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("S,dh", [(130, 64), (130, 128), (600, 64), (600, 32), (640, 128)])
+@pytest.mark.parametrize("which,value", [(0, np.inf), (0, np.nan), (1, -np.inf), (1, np.nan), (2, np.inf), (2, np.nan), (3, np.inf), (3, np.nan)])
+def test_infinities_stay_to_the_end(K, dtype, S, dh, which, value):
+    """q, k, v or dout with one bad column in one row: every output that has it in a sum is an infinity or a NaN, in later chunks and segments too."""
+    at, col, H = 77, 5, 2
+    case = Case(dtype, 1, S, H, dh, seed=4)
+    (case.dout if which == 3 else case.qkv)[at, (0 if which == 3 else which * H * dh) + col] = value       # head 0
+    d = case.upload()
+    case.outputs()
+    case.forward(K)
+    case.backward(K)
+    out = {n: d[n].float().cpu().numpy() for n in ("o", "dqkv")}
+    w = H * dh
+    outs = {"o": out["o"][:, :dh], **{n: out["dqkv"][:, i * w:i * w + dh] for i, n in enumerate(("dq", "dk", "dv"))}}
+    every, one, before, here, after = slice(None), col, slice(0, at + 1), slice(at, at + 1), slice(at, S)
+    bad = [dict(o=(here, every), dk=(before, one), dv=(before, every)), dict(o=(after, every), dq=(after, one), dv=(here, every)),
+           dict(o=(after, one), dq=(after, every), dk=(here, every)), dict(dq=(here, every), dk=(before, every), dv=(before, one))][which]
+    for n, where in bad.items():
+        assert not np.isfinite(outs[n][where]).any(), n
+    states = {0: d["ds0"], 1: d["s_out"], 2: d["s_out"], 3: d["ds0"]}[which].cpu().numpy()[0, 0]
+    assert not np.isfinite(states[col] if which in (0, 1) else states[:, col]).any()

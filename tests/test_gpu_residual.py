@@ -495,3 +495,31 @@ def test_8_bit_rows_with_an_infinity(K):
     K.lpk_rmsnorm_fwd(0, b.dev(np.ones((1, 64), np.float32)), None, b.dev(g), None, None, y8, s8, None, 1, 64, 1e-5)
     got = host(y8)[0]
     assert np.isnan(got[7]) and not np.delete(got, 7).any() and np.isinf(host(s8)[0])
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("rows,d", [(70001, 24), (35001, 100), (17001, 200), (8199, 449), (8195, 768), (12300, 1001), (2500, 2047), (2501, 2048), (2500, 4096),
+                                    (700, 8191), (600, 8192), (301, 9001), (301, 16384)])
+def test_norm_backward_of_several_rows_a_block(K, dtype, shift, rows, d):
+    """Two to four rows one after another in a block's turn, the last turn not full: their gain's gradient, the loads ahead, the numbers drawn again."""
+    norm_case(K, dtype, rows, d, 0.25, True, shift, seed=4)
+
+
+def test_norm_gain_gradient_beyond_32_bit_offsets(K):
+    import torch
+    rows, d = 262400, 8200
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(rows, d, device="cuda", generator=gen, dtype=torch.bfloat16)
+    dy = torch.randn(rows, d, device="cuda", generator=gen, dtype=torch.bfloat16)
+    rstd = torch.rand(rows, device="cuda", generator=gen) + 0.5
+    g, dg = torch.ones(d, device="cuda"), torch.empty(d, device="cuda")
+    K.lpk_rmsnorm_bwd(1, dy, x, rstd, g, None, None, None, dg, rows, d, 0, torch.empty(K.lpk_rmsnorm_scratch(rows, d), device="cuda"))
+    want, size = (torch.zeros(d, device="cuda", dtype=torch.float64) for _ in range(2))
+    for a in range(0, rows, 8192):
+        t = dy[a:a + 8192].double() * x[a:a + 8192].double() * rstd[a:a + 8192, None].double()
+        want += t.sum(0)
+        size += t.abs().sum(0)
+    # sums one after another in each of 1024 blocks, then in 64 groups: 2^-24 of the partial sums for each of the steps of a chain, which are independent
+    steps = rows / 1024 + 1024 / 64 + 64
+    assert bool(((dg - want).abs() <= 2.0 ** -24 * (8 + steps ** 0.5) * size).all())
