@@ -12,7 +12,8 @@
 //
 // Products run on the matrix cores, 32 x 32 tiles.  A wave keeps 32 columns of the state, all rows of them, in fp32 accumulators, and
 // the waves of a head share the chunk's q, k and v through LDS.  The accumulators' layout is that of an operand whose reduction
-// index is the row, so that the state and the scores K Q^T go from one product to the next without leaving the registers.
+// index is the row, so that the state and the scores K Q^T go from one product to the next without leaving the registers (but for fp32 heads of
+// 65 to 96, where the compiler puts 48 to 164 bytes a lane into scratch memory, and bf16 heads of 97 to 128 with a final state, 32).
 // Heads of up to 64: two waves for every 32 columns, one with the state, which multiplies it with the chunk's queries and then
 // adds the chunk to it, and one with the chunk's own scores and their product with the values, which adds both parts of the output.
 // Wider heads, whose state fills the registers anyway: one wave does both.
@@ -236,8 +237,8 @@ struct LinearShape {
 
 // What a block works on: its job, sequence, head and stretch of positions.
 struct Place {
-  int job, seg, bh, h, len, first, last, stop, units;
-  size_t row0, row;            // the sequence's first row; the row of position 0 in the job's direction
+  int job, seg, bh, h, len, first, last, stop;
+  size_t row0;                 // the sequence's first row
   float g2;
 };
 // Blocks go to the eight dies by turns of their number, x first: the jobs (y) of one segment, which share its rows, run on one die.
@@ -297,8 +298,8 @@ __device__ __forceinline__ void scale(f32x16 (&state)[ND], float by) {
 }
 
 // Between the rows of a tile: 16 bytes spread what a wave reads of 32 neighbouring rows or of 4 rows, 64 bytes each, over the banks,
-// but for 128 bf16, which are the banks' period (the walk there, 32 heads of 2048 positions, forward and backward: 50 + 88 us with 16 bytes, 49 + 86 with
-// 80; its states kernel, whose blocks hold twice the rows, loses by them, 53 + 91).
+// but for 128 bf16, which are the banks' period (1024 heads of 1024 positions, forward and backward: 358 + 1017 us with 16 bytes in the walk, 357 + 1009 with
+// 80; the states kernel, whose blocks hold twice the rows, loses by them: 32 heads of 2048 positions 56.5 + 104 with 16, 59 + 107 with 80).
 template <typename T> constexpr int kPad = 16 / (int)sizeof(T);
 template <typename T, int DK> constexpr int kWalkPad = sizeof(T) == 2 && DK == 128 ? 40 : kPad<T>;
 template <typename T, int DK>
@@ -308,19 +309,20 @@ struct WalkLds {
   Tile<T, DK> t[2];
   __attribute__((aligned(16))) float weight[2][kChunk];             // of whole chunks, and of the last
   int bad[2];
-  f32x4 earlier[2][DK <= 64 ? DK / 32 : 1][4][64];                  // two roles, by turns: as the accumulators hold it
+  f32x4 earlier[2][DK <= 64 ? DK / 32 : 1][4][64];                  // two roles, by turns: as the accumulators hold it (one role: not used)
 };
 
-// Waves for 32 columns: two of up to 64 wide heads (64 wide, 96 heads, 1024 positions, cut: 17.5 us with one, 15.1 with two),
-// one of wider ones (128 wide, 1024 heads of 1024 positions, forward: 300 us with one, 332 with two).
+// Waves for 32 columns: two of up to 64 wide heads (96 heads of 64, 1024 positions, forward: 32 us; with one, which does not fit the registers of three waves a
+// SIMD, 48), one of wider ones, forward and backward, us, one and two: bf16, 128 wide, 1024 heads of 1024 positions 357 + 1009 and 369 + 1060, 32 heads of 2048
+// 56.5 + 104 and 59.5 + 111, but 64 heads 81 + 193 and 86 + 146; fp32, which two would suit, 40 heads of 2048 136 + 356 and 124 + 322.
 template <int DK> constexpr int kRoles = DK <= 64 ? 2 : 1;
 template <typename T, int DK> constexpr int kWavesPerSimd = DK <= 64 ? 3 : sizeof(T) * DK == 512 ? 1 : 2;
 
-// A block: one segment of one head.  bf16, a walk alone: 16 heads of 64, 16384 positions, cut, 33.8 us (134 MB of tensors, 4 TB/s); 96 heads of 1024
-// positions 15.1 us cut (3.3 TB/s), its three backward jobs uncut 51.6 (88 MB).  Where the card is full, memory bounds it (512 heads of
-// 1024 positions: forward 60 us, 4.4 TB/s); where it is not, the wave with the state, for which a chunk takes about 3000 clocks, one step waiting for
-// the other: LDS, splitting the state, products, LDS.  Two such waves with half of the rows each gained a sixth of
-// that and lost more to the wider blocks (16 heads of 16384: 52 + 98 us became 57 + 106).
+// A block: one segment of one head.  bf16, a walk alone: 16 heads of 64, 16384 positions, cut, 35 us (134 MB of tensors, 3.8 TB/s); 96 heads of 1024
+// positions 17 us cut (3 TB/s), its three backward jobs uncut 61 to 66 (88 MB).  Where the card is full, memory bounds it (512 heads of
+// 1024 positions: forward 63 us, 4.3 TB/s); where it is not, the wave with the state, for which a chunk takes about 3500 clocks, one step waiting for
+// the other: LDS, splitting the state, products, LDS.  Two such waves with half of the rows each gained a sixth of that and lost more to the wider
+// blocks (with two bf16 parts a value instead of three, 16 heads of 16384: 52 + 98 us became 57 + 106).
 template <typename T, int DK, bool VEC, bool FIN>
 __global__ void __launch_bounds__(2 * kRoles<DK> * DK, (kWavesPerSimd<T, DK>)) k_linear_walk(LinearJobs jobs, LinearShape sh, int units) {
   constexpr int ROLES = kRoles<DK>, NT = 2 * ROLES * DK, NP = kParts<T>, ND = DK / 32;
@@ -593,7 +595,7 @@ struct StateJob {
 struct StateJobs { StateJob j[2]; };
 
 // Two waves for every 32 columns, which take a half of every 64 positions each; their sums are added at the end.  16 heads of 64, 16384
-// positions, bf16: 23.3 us for the 67 MB of k and v, 2.9 TB/s.
+// positions, bf16: 22 us for the 67 MB of k and v, 3 TB/s.
 template <typename T, int DK, bool VEC>
 __global__ void __launch_bounds__(4 * DK) k_linear_states(StateJobs jobs, LinearShape sh, int units) {
   constexpr int ND = DK / 32, LD = DK + kPad<T>, R = 2 * kChunk;
@@ -717,7 +719,7 @@ __global__ void __launch_bounds__(256) k_linear_scan(StateJobs jobs, LinearShape
 
 // One position, a block for each head: the state is read, decayed, added to and written back in one pass, four neighbouring elements a thread and
 // four rows of them in flight.  Bound by the state's bytes (192 sequences of 16 heads of 64, bf16: 16.8 us for 101 MB, of which the last-level cache holds a part:
-// 6 TB/s), with few heads by the launch (12 heads: 3.6 us).
+// 6 TB/s), with few heads by the launch (12 heads: 3.7 us).
 template <typename T>
 __global__ void __launch_bounds__(256) k_linear_step(const T* __restrict__ qkv, const float* __restrict__ log_decay, float* __restrict__ state,
                                                      T* __restrict__ o, int H, int dh, float scale) {
@@ -780,14 +782,21 @@ __global__ void __launch_bounds__(256) k_linear_step(const T* __restrict__ qkv, 
 
 constexpr int kMaxHead = 128;
 
-// Segments of a sequence: as many as make one round of the blocks that run at once (three a compute unit up to 64 wide, two of wider heads, one in
-// fp32 beyond 96, whose registers hold no second one; there two rounds where one would be less than three segments), but none of less than four chunks, and no
-// cut into two, which costs two more launches and a second pass over k and v.  Forward and backward, us:
-//   16 heads of 64, 16384 positions, for 384 / 768 / 1024 blocks     57 + 127, 54 + 100, 60 + 117;  96 heads, 1024 positions  31 + 48, 31 + 49, 31 + 53
-//   32 heads of 128, 2048 positions, for 256 / 512 / 768 blocks      49 + 156, 52 + 83, 50 + 86;    128 heads  162 + 249, 115 + 250, 137 + 250
-//   the same in fp32, 40 heads 134 + 507, 153 + 355, 168 + 351;      80 heads  251 + 518, 267 + 518, 296 + 663
+// Segments of a sequence: as many as make three blocks a compute unit up to 64 wide, two of wider heads, one in fp32 beyond 96 (there two where one would be less
+// than three segments), but none of less than four chunks, and no cut into two, which costs two more launches and a second pass over k and v.  Three, two and one
+// are what runs at once in bf16 beyond 32 and in fp32 beyond 96; up to 32 wide LDS holds six blocks in bf16 and four in fp32, in fp32 33 to 64 wide two and
+// 65 to 96 wide one.  Whole calls, forward and backward, us:
+//   blocks of 64 wide heads, 384 / 768 / 1024     bf16  16 heads, 16384 positions  67 + 147, 60 + 116, 65 + 129;  96 heads, 1024 positions  32 + 56, 32 + 56, 32 + 58
+//                                                 fp32  32 heads, 2048 positions  49 + 95, 41 + 82, 41 + 97
+//   of 32 wide heads, 384 / 768 / 1024            bf16  32 heads, 2048 positions  20 + 33, 19 + 24, 19 + 26;  16 heads, 16384 positions  44 + 98, 41 + 59, 32 + 72
+//                                                 fp32  31 + 59, 25 + 39, 25 + 39;  83 + 204, 57 + 119, 52 + 100
+//   of 128 wide heads, 256 / 512 / 768            bf16  32 heads, 2048 positions  53 + 190, 56 + 104, 58 + 102;  128 heads  206 + 291, 137 + 291, 161 + 292
+//                                                 fp32  40 heads  134 + 507, 153 + 355, 168 + 351;  80 heads  251 + 518, 267 + 518, 296 + 663
+//   of 96 wide heads, 256 / 512 / 768             40 heads, 2048 positions  bf16  54 + 173, 49 + 87, 55 + 99;  fp32  136 + 571, 149 + 361, 154 + 351
 //   of four chunks at least, or two: 32 heads of 64 in fp32, 2048 positions, forward 42 and 55; or six: 35 heads in fp32, 511 positions, which are
-//   then not cut, 25 and 42;  in two: 8 heads of 64, 300 positions 16 + 17, uncut 14 + 14
+//   then not cut, 25 and 42
+//   uncut, or in two: 8 heads of 64, 300 positions 16 + 16, 19.5 + 20; 96 heads of 64, 1024 positions, backward 56.6, 57.2; 64 heads of 128, 2048 positions,
+//   backward 193, 177; 80 of them in fp32 517, 693
 struct Cut { int segments, per; };
 Cut cut_of(int dt, int B, int S, int H, int dh, int jobs) {
   const int chunks = (S + kChunk - 1) / kChunk, alone = dt == F32 && dh > 96;

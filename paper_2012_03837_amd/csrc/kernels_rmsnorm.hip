@@ -3,15 +3,15 @@
 //   forward :  r = drop(x) (+ res),  rstd = (mean r^2 + eps)^-1/2,  y = r rstd g;  8 bits: y8 = e4m3(y / s), s = max |y| / 448
 //   backward:  a = g dy,  dres = rstd (a - r rstd^2 mean(a r)) (+ add),  dx = drop'(dres),  dg = sum over rows of dy r rstd
 // All are bound by memory: every tensor is read or written once, 16 bytes a lane, with the row in registers between its sums and
-// its outputs.  A row belongs to LPR neighbouring lanes (8 to 64: rows of up to 512 elements fill a wave with several of them, as
-// the norm over a head needs) or to a block of 256 to 1024 threads.  Eight neighbouring elements a lane and step; where the
+// its outputs.  A row belongs to LPR neighbouring lanes (8 to 32 up to 256 elements, so that several rows share a wave, as the norm over a head
+// needs; 64, a wave, up to 1024) or to a block of 256 to 1024 threads.  Eight neighbouring elements a lane and step; where the
 // width or an address is no multiple of them (ODD) the same accesses stand anywhere and a row's last ones are taken singly.
 // What they take, bf16 (tensors' bytes over the time; 8192 rows of 4096 are 67 MB a tensor):
 //   dropout and addition, 8192 x 4096, and its gradient   63.9 us, 5.2 TB/s (335 MB)
-//   forward, dropout, addition, 8192 x 768                13.9 us, 3.6 TB/s; with 8-bit output, 8192 x 4096, 46.4 us, 5.1 TB/s
-//   backward, 8192 x 768                                  15.0 us, 4.2 TB/s, and 3.9 us for the sum of dg
+//   forward, dropout, addition, 8192 x 768                13.6 us, 3.7 TB/s; with 8-bit output, 8192 x 4096, 46 us, 5.1 TB/s
+//   backward, 8192 x 768                                  14.7 us, 4.3 TB/s, and 4.0 us for the sum of dg
 //   4 rows of 1024                                        3.1 us: the launch
-// A copy of 4 GB reaches 4.85 TB/s here; tensors of some 10 MB end before the loads are in full flight.
+// A copy of 4 GB reaches 4.85 TB/s here, less than what reads more than it writes; tensors of some 10 MB end before the loads are in full flight.
 #include "common.h"
 #include "philox.h"
 
@@ -272,7 +272,9 @@ __global__ void __launch_bounds__(threads_of(LPR)) k_rms_fwd(const T* x, const T
 }
 
 // Blocks walk over the rows with a stride and keep the sums of dg of their columns in registers; partial[block][d].  A row stays in
-// registers as it was loaded, and where that is little enough the next one's loads are under way beside it.
+// registers as it was loaded, and where that is little enough the next one's loads are under way beside it.  Where it is not, the compiler
+// puts a few of them into scratch memory, bytes a lane: bf16 of odd widths 12 from 2049 on, 28 from 4097 on, 44 from 8193 on; fp32 28 for 2049 to 4096 and 52
+// from 8193 on, of odd widths 20 for 513 to 1024, 44 from 2049 on, 68 from 4097 on, 88 from 8193 on.
 template <typename T, int LPR, int NCH, bool ODD>
 __global__ void __launch_bounds__(threads_of(LPR), 4) k_rms_bwd(const T* dy, const T* r, const float* __restrict__ rstd,
                                                              const float* __restrict__ g, const T* add, T* dres, T* dx,
