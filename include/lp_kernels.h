@@ -137,6 +137,53 @@ int lpk_rmsnorm_bwd(int dtype, const void* dy, const void* r, const float* rstd,
                     float* scratch_dev, size_t scratch_elems, void* stream);
 size_t lpk_rmsnorm_scratch(int rows, int d);
 
+/* Rotary positions of the heads of a matrix's rows, for training (on the q and k columns of qkv in front of lpk_attention_fwd; the
+ * backward call on those of dqkv) and for single tokens: with t = pos freq[i], of the pair (a, b) = columns (i, i + rot/2) of a head, or (2 i, 2 i + 1)
+ * if `interleaved`, i < rot/2,
+ *   y = scale (a cos t - b sin t, a sin t + b cos t);      backward: the transpose, the gradient of x from that of y.
+ * x and y: `rows` rows of heads * dh columns (dh up to 512) with leading dimensions ldx and ldy; columns rot .. dh - 1 of a head (rot even) are copied;
+ * y may be x (ldy = ldx), otherwise they do not overlap.  pos int32 [rows] on the device, any number (null: row % S); freq fp64 [rot/2] on
+ * the device, radians a position: the product is taken in 64 bits.  rows up to 2^30, heads * dh up to 2^24, leading dimensions to 2^32.
+ * lpk_rotary_frequencies writes such a table to host memory: base^(-2 i / rot), stretched for contexts longer than those trained on: divided by
+ * `factor` where a pair turns at most `low` times within `context` positions, kept where it turns `high` times or more, in between blended in the number of
+ * turns (factor 1: kept; low = high = infinity: all divided). */
+int lpk_rotary(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const int32_t* pos, const double* freq, int rows, int S, int heads,
+               int dh, int rot, int interleaved, float scale, int backward, void* stream);
+int lpk_rotary_frequencies(double* freq, int rot, double base, double factor, double low, double high, double context);
+
+/* A paged cache of keys and values in 8 bits (e4m3) with a scale for each page and head, written by lpk_cache_append, read back
+ * by lpk_cache_read and attended over by lpk_cache_attention.
+ * A page holds `page` tokens (16, 32, 64, 128 or 256): kpages [n_pages, Hkv, page, dh], vpages [n_pages, Hkv, dh, page] (16-byte aligned), kscale and
+ * vscale fp32 [n_pages, Hkv]; dh a multiple of 16 up to 256.  table int32 [B, max_pages] (max_pages * page up to 2^30): page number of
+ * each `page` positions of a sequence; a number outside 0 .. n_pages - 1 means that there is no page: nothing is written there, zeros are read, and
+ * attention sees no token there.  lens int32 [B]: the sequences' lengths, those of the call's new rows included, taken as 0 .. max_pages * page.
+ * The new rows of sequence b are rows starts[b] .. starts[b + 1] - 1 (starts int32 [B + 1]; null: rows b T .. b T + T - 1), and n of them stand at its
+ * positions lens[b] - n .. lens[b] - 1.  T: at most so many rows a sequence; one whose rows are more, not in order or not within the `rows` rows of
+ * the matrix counts as one of none.  Rows of no sequence are neither read nor written.  All of these are on the device, B up to 2^20.
+ *
+ * Append quantises rows of k and v (compute dtype, Hkv * dh columns, leading dimensions ldk and ldv): per page and head s' = max(s, need), need the least power
+ * of two (2^-126 at least) with |x| / need <= 448 for all new finite x, s the scale of the page's earlier tokens (positions before the new rows'; none: s' =
+ * need); code = e4m3(x / s'), rounded to nearest even, and where s' > s the earlier codes become e4m3(code s / s').  A NaN or an infinity is held as
+ * a NaN and has no part in the scale.  Two sequences of one call write to different pages.
+ * Read writes code * s of the same rows to k and v (zeros for positions before the first).
+ *
+ * Attention: o = softmax(q k^T dh^-1/2) v for the rows of q [rows, H * dh] (leading dimension ldq; H a multiple of Hkv, heads h G .. h G + G - 1 read
+ * head h of the cache, G = H / Hkv), over the positions up to the row's own if `causal`, otherwise all of the sequence's.  o [rows, H * dh]; lse fp32 [rows, H]
+ * (may be null) = log-sum-exp of the scaled scores.  A row that sees no token becomes zeros, its lse minus infinity.  What a row does not see does not
+ * change it, a NaN there included.  q and o do not overlap.  scratch_dev: lpk_cache_attention_scratch floats (needs no device; may be 0), 16-byte aligned; contents
+ * undefined on return, so that calls which share it are ordered. */
+int lpk_cache_append(int dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, int rows, const int32_t* starts, const int32_t* lens,
+                     const int32_t* table, void* kpages, void* vpages, float* kscale, float* vscale, int B, int T, int Hkv, int dh, int page,
+                     int max_pages, int n_pages, void* stream);
+int lpk_cache_read(int dtype, void* k, int64_t ldk, void* v, int64_t ldv, int rows, const int32_t* starts, const int32_t* lens,
+                   const int32_t* table, const void* kpages, const void* vpages, const float* kscale, const float* vscale, int B, int T, int Hkv,
+                   int dh, int page, int max_pages, int n_pages, void* stream);
+int lpk_cache_attention(int dtype, const void* q, int64_t ldq, int rows, const int32_t* starts, const int32_t* lens, const int32_t* table,
+                        const void* kpages, const void* vpages, const float* kscale, const float* vscale, void* o, int64_t ldo, float* lse, int B,
+                        int T, int H, int Hkv, int dh, int page, int max_pages, int n_pages, int causal, float* scratch_dev, size_t scratch_elems,
+                        void* stream);
+size_t lpk_cache_attention_scratch(int B, int T, int H, int Hkv, int dh, int page, int max_pages);
+
 /* LayerNorm over the last dimension (eps 1e-5, biased variance); backward adds `add` to dx if given. */
 int lpk_layernorm_fwd(int dtype, const void* x, const float* g, const float* b, void* y, float* mean, float* rstd,
                       int rows, int d, void* stream);

@@ -1,0 +1,583 @@
+// Attention over the 8-bit cache (cache.h has the layout): o = softmax(q k^T dh^-1/2) v over a sequence's positions, without or with those
+// behind the row's own.
+//
+// The rows of a sequence that read one head of the cache, n new tokens times the G query heads that share it, are the columns of a tile;
+// 64 tokens of the cache are its rows.  A wave keeps both products transposed, on the 16 x 16 x 32 matrix instruction:
+//   S^T[token, column] = K Q^T,   O^T[dh, column] += V^T P^T
+// Lane l has column l % 16 of S^T; which tokens the rows of K stand for is free, and they are dealt so that the lane's sixteen
+// scores belong to the tokens 16 (l / 16) .. + 15, in order: what it then needs of V^T for each of its columns of a head is one access of sixteen bytes, the operand of
+// two products, and sixteen tokens never leave a page, so that a lane has one page, one scale of the keys and one of the
+// values.  Neither scores nor weights go through LDS.
+// Codes become bf16 by one conversion instruction, exactly.  The scales multiply scores and weights in fp32.  Weights enter the second
+// product as the sum of two bf16 parts (three where the call is in fp32, whose queries are cut in three as well): what is left out is 2^-16 of a weight (2^-24), so
+// that an output is off by its own rounding and no more; the products are not what bounds the calls that read the cache once.
+#include <type_traits>
+
+#include "cache.h"
+
+namespace lp {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kWaves = 4;                                  // of a block, each with every fourth tile of 64 tokens
+
+struct AttnArgs {
+  const void* q;
+  void* o;
+  float *lse, *part;        // part: what the pieces of a divided axis leave
+  int64_t ldq, ldo;
+  int H, G, causal, tiles;  // tiles: column tiles of a sequence, at most
+  int target;               // pieces that the axes are divided into, about (0: none is divided)
+  bool vec;
+  float scale;
+};
+
+__device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+// Eight codes, as the numbers they are.
+__device__ __forceinline__ bf16x8 codes8(unsigned a, unsigned b) {
+  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
+  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
+  bf16x8 v;
+  v[0] = p[0]; v[1] = p[1]; v[2] = q[0]; v[3] = q[1]; v[4] = r[0]; v[5] = r[1]; v[6] = s[0]; v[7] = s[1];
+  return v;
+}
+// Eight numbers as sums of N bf16 parts, each the nearest to what the ones before leave: two leave 2^-16 of a number, three nothing.
+template <int N>
+__device__ __forceinline__ void split8(float (&r)[8], bf16x8 (&f)[N]) {
+#pragma unroll
+  for (int s = 0; s < N; ++s) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[s][e] = (bf16_t)r[e];
+    if (s + 1 < N) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e] -= (float)f[s][e];
+    }
+  }
+}
+// 0xff where a byte is a NaN's code.
+__device__ __forceinline__ unsigned nan_bytes(unsigned w) {
+  const unsigned hit = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  return (hit >> 7) * 0xffu;
+}
+
+// What a block works on.
+struct Work { int b, h, tile, piece, pieces, slot; };
+
+// Sum over the block's threads of two numbers, and of those before the thread's own.
+struct Two { unsigned long long a, b; };
+__device__ __forceinline__ Two scan(Two v, Two* before, Two* sh) {
+  Two run = v;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned long long a = __shfl_up(run.a, o, 64), b = __shfl_up(run.b, o, 64);
+    if (lane >= o) { run.a += a; run.b += b; }
+  }
+  __syncthreads();
+  if (lane == 63) sh[wave] = run;
+  __syncthreads();
+  Two base = {0, 0}, all = {0, 0};
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) { base.a += sh[w].a; base.b += sh[w].b; }
+    all.a += sh[w].a;
+    all.b += sh[w].b;
+  }
+  if (before) *before = Two{base.a + run.a - v.a, base.b + run.b - v.b};
+  return all;
+}
+
+// The axes are cut so that all pieces have the same number of tiles, whatever the sequences' lengths: `each` tiles a piece, as
+// many as leave about `target` pieces in all.  Pieces are numbered through sequences, heads, column tiles and the axis; the block finds
+// number `id` (or, by pair, the first piece of pair `id` of (sequence, head, column tile)).  slot: place of the result among those of divided axes, at
+// most 2 target of them.
+__device__ __forceinline__ bool find_work(const CacheView& c, const AttnArgs& a, int width, int64_t id, bool by_pair, Work* w) {
+  if (a.target == 0 || by_pair) {
+    const int64_t rest = id / a.tiles;
+    w->tile = (int)(id % a.tiles);
+    w->h = (int)(rest % c.Hkv);
+    w->b = (int)(rest / c.Hkv);
+    w->piece = w->slot = 0;
+    w->pieces = 1;
+    if (w->b >= c.B) return false;
+    if (a.target == 0) return true;
+  }
+  __shared__ Two sh[kWaves];
+  __shared__ Work found;
+  const int each_thread = (c.B + 255) / 256, from = threadIdx.x * each_thread, to = from + each_thread < c.B ? from + each_thread : c.B;
+  auto size_of = [&](int b, int* tiles) {                    // of a head: column tiles, and tiles of the axis
+    const Sequence s = sequence_of(c, b);
+    *tiles = (s.len + 63) >> 6;
+    return (int)(((int64_t)s.n * a.G + width - 1) / width);
+  };
+  Two sum = {0, 0};
+  for (int b = from; b < to; ++b) {
+    int tiles;
+    const int columns = size_of(b, &tiles);
+    sum.a += (unsigned long long)columns * tiles;
+  }
+  const unsigned long long all = scan(sum, nullptr, sh).a * c.Hkv;
+  unsigned long long each = (all + a.target - 1) / a.target;
+  if (each < kWaves) each = kWaves;
+  sum = Two{0, 0};
+  auto pieces_of = [&](int tiles) { return tiles > 0 ? (int)((tiles + each - 1) / each) : 1; };
+  for (int b = from; b < to; ++b) {
+    int tiles;
+    const unsigned long long pairs = (unsigned long long)size_of(b, &tiles) * c.Hkv;
+    const int pieces = pieces_of(tiles);
+    sum.a += pairs * pieces;
+    sum.b += pieces > 1 ? pairs * pieces : 0;
+  }
+  Two at;
+  const Two total = scan(sum, &at, sh);
+  if (!by_pair && (unsigned long long)id >= total.a) return false;
+  for (int b = from; b < to; ++b) {
+    int tiles;
+    const int columns = size_of(b, &tiles), pieces = pieces_of(tiles);
+    const unsigned long long n = (unsigned long long)columns * c.Hkv * pieces;
+    const bool mine = by_pair ? b == w->b : (unsigned long long)id >= at.a && (unsigned long long)id < at.a + n;
+    if (mine) {
+      const unsigned long long i = by_pair ? ((unsigned long long)w->h * columns + w->tile) * pieces : id - at.a;
+      found.b = b;
+      found.piece = (int)(i % pieces);
+      found.tile = columns ? (int)(i / pieces % columns) : 0;
+      found.h = columns ? (int)(i / pieces / columns) : 0;
+      found.pieces = by_pair && w->tile >= columns ? 1 : pieces;
+      found.slot = (int)(at.b + i);
+    }
+    at.a += n;
+    at.b += pieces > 1 ? n : 0;
+  }
+  __syncthreads();
+  if (by_pair) {
+    w->pieces = found.pieces;
+    w->slot = found.slot;
+  } else {
+    *w = found;
+  }
+  return true;
+}
+// Tiles of a piece: [first, last).
+__device__ __forceinline__ void tiles_of(int tiles, int piece, int pieces, int* first, int* last) {
+  const int each = (tiles + pieces - 1) / pieces;
+  *first = piece * each;
+  *last = *first + each < tiles ? *first + each : tiles;
+}
+
+// A column's row of q and o, and its head's first column there.
+struct Column { int64_t row; int head, t; bool there; };
+__device__ __forceinline__ Column column_of(const Sequence& s, const AttnArgs& a, int h, int col) {
+  Column c;
+  c.t = col / a.G;
+  c.there = c.t < s.n;
+  c.row = s.first + c.t;
+  c.head = h * a.G + col - c.t * a.G;
+  return c;
+}
+
+template <typename T>
+__device__ __forceinline__ void put4(T* p, f32x4 v, bool vec) {
+  if constexpr (std::is_same<T, float>::value) {
+    if (vec) { *reinterpret_cast<f32x4*>(p) = v; return; }
+  } else {
+    bf16x4 t;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = (bf16_t)v[e];
+    if (vec) { *reinterpret_cast<bf16x4*>(p) = t; return; }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) p[e] = from_f<T>(v[e]);
+}
+// The end of a row: its sum of weights l (negative: all its scores are minus infinity), their maximum m in powers of two.  No token: zeros.
+__device__ __forceinline__ float over(float m, float l) {
+  if (m == -INFINITY && l == 0.f) return 0.f;                        // times this, the sums are zeros
+  return l < 0.f ? __builtin_bit_cast(float, 0x7fc00000u) : 1.f / l;
+}
+__device__ __forceinline__ float log_sum(float m, float l) { return m == -INFINITY && l <= 0.f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2; }
+
+// ND: head size in units of 64 columns, rounded up.  NC: column tiles of 16.
+template <typename T, int ND, int NC>
+__global__ void __launch_bounds__(64 * kWaves) k_cache_attn(CacheView c, AttnArgs a) {
+  constexpr int QP = std::is_same<T, float>::value ? 3 : 1, WP = std::is_same<T, float>::value ? 3 : 2, NJ = 4 * ND;
+  constexpr int kPad = 64 * ND + 4;
+  // the queries, and when the axis is done what waves hand to each other
+  constexpr int kQueries = NC * ND * 2 * QP * 64 * 16, kJoin = kWaves / 2 * 16 * (kPad + 2) * 4;
+  __shared__ __align__(16) char lds[kQueries > kJoin ? kQueries : kJoin];
+  auto sq = reinterpret_cast<bf16x8(*)[64]>(lds);
+  auto so = reinterpret_cast<float(*)[16][kPad]>(lds);
+  auto sml = reinterpret_cast<float(*)[2][16]>(lds + kWaves / 2 * 16 * kPad * 4);
+  Work w;
+  if (!find_work(c, a, 16 * NC, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, false, &w)) return;
+  const Sequence s = sequence_of(c, w.b);
+  const int col0 = w.tile * 16 * NC;
+  if ((int64_t)col0 >= (int64_t)s.n * a.G) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+  const int dh = c.dh, page = 1 << c.shift;
+
+  // queries, as they enter the products
+  for (int f = wave; f < NC * ND * 2; f += kWaves) {
+    const int half = f & 1, cc = f / 2 % ND, n = f / (2 * ND), d = cc * 64 + g * 16 + half * 8;
+    const Column col = column_of(s, a, w.h, col0 + n * 16 + i);
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (col.there && d < dh) {
+      const T* p = (const T*)a.q + col.row * a.ldq + col.head * dh + d;
+      if (a.vec) {
+        if constexpr (QP == 1) {
+          const bf16x8 t = *reinterpret_cast<const bf16x8*>(p);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
+        } else {
+          const f32x4 t = *reinterpret_cast<const f32x4*>(p), u = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { v[e] = t[e]; v[4 + e] = u[e]; }
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = to_f(p[e]);
+      }
+    }
+    bf16x8 parts[QP];
+    split8<QP>(v, parts);
+#pragma unroll
+    for (int q = 0; q < QP; ++q) sq[f * QP + q][lane] = parts[q];
+  }
+  __syncthreads();
+
+  // visible tokens of the lane's columns (0: none), of the first and of the last column there is
+  int lim[NC], lo, hi;
+  {
+    const int most = s.n * a.G - 1, end = col0 + 16 * NC - 1 < most ? col0 + 16 * NC - 1 : most;
+    auto limit = [&](int t) {
+      const int v = a.causal ? s.len - s.n + t + 1 : s.len;
+      return v < 0 ? 0 : v;
+    };
+    lo = limit(col0 / a.G);
+    hi = limit(end / a.G);
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      const Column col = column_of(s, a, w.h, col0 + n * 16 + i);
+      lim[n] = col.there ? limit(col.t) : 0;
+    }
+  }
+  int tile, last;
+  tiles_of((((a.target ? s.len : hi) + 63) >> 6), w.piece, w.pieces, &tile, &last);
+  if (last > (hi + 63) >> 6) last = (hi + 63) >> 6;
+
+  f32x4 acc[NC][NJ];
+  float m[NC], l[NC];
+  bool seen[NC];
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    m[n] = -INFINITY;
+    l[n] = 0.f;
+    seen[n] = false;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  for (tile += wave; tile < last; tile += kWaves) {
+    const int tok = tile * 64, kt = tok + 16 * (i >> 2), vt = tok + 16 * g;
+    const int pk = kt < hi ? page_of(c, w.b, kt >> c.shift) : -1, pv = vt < hi ? page_of(c, w.b, vt >> c.shift) : -1;
+    uint4 kr[4][ND], vr[NJ];
+    {
+      const uint8_t* p = c.k + ((((int64_t)(pk < 0 ? 0 : pk) * c.Hkv + w.h) << c.shift) + (kt & (page - 1)) + (i & 3)) * dh;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int cc = 0; cc < ND; ++cc) {
+          const int d = cc * 64 + g * 16;
+          kr[t][cc] = pk >= 0 && d < dh ? *reinterpret_cast<const uint4*>(p + t * 4 * dh + d) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    float ks = 0.f, vs = 0.f;
+    {
+      const int64_t where = (int64_t)(pv < 0 ? 0 : pv) * c.Hkv + w.h;
+      const uint8_t* p = c.v + ((where * dh + i) << c.shift) + (vt & (page - 1));
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) vr[j] = pv >= 0 && j * 16 < dh ? *reinterpret_cast<const uint4*>(p + (j * 16 << c.shift)) : make_uint4(0, 0, 0, 0);
+      if (pv >= 0) {
+        ks = c.ks[where] * a.scale;
+        vs = c.vs[where];
+      }
+    }
+    const bool masked = tok + 64 > lo || __ballot(pv < 0) != 0;
+
+    f32x4 sc[NC][4];
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) sc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int cc = 0; cc < ND; ++cc)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        bf16x8 kf[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) kf[t] = half ? codes8(kr[t][cc].z, kr[t][cc].w) : codes8(kr[t][cc].x, kr[t][cc].y);
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+          for (int q = QP - 1; q >= 0; --q) {
+            const bf16x8 qf = sq[((n * ND + cc) * 2 + half) * QP + q][lane];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sc[n][t] = mma(kf[t], qf, sc[n][t]);
+          }
+      }
+
+    bf16x8 wf[NC][2][WP];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float x = sc[n][t][r] * ks;
+          if (masked) {
+            const bool ok = vt + t * 4 + r < lim[n] && pv >= 0;
+            x = ok ? x : -INFINITY;
+            seen[n] |= ok;
+          }
+          sc[n][t][r] = x;
+          top = fmaxf(top, x);
+        }
+      if (!masked) seen[n] = true;
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      top = fmaxf(top, m[n]);
+      const float base = top == -INFINITY ? 0.f : top;
+      if (__ballot(top > m[n])) {
+        const float f = __builtin_amdgcn_exp2f(m[n] - base);
+        l[n] *= f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[n][j] *= f;
+        m[n] = top;
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(sc[n][2 * half + e / 4][e % 4] - base);
+          l[n] += p[e];
+          p[e] *= vs;
+        }
+        split8<WP>(p, wf[n][half]);
+      }
+    }
+
+    if (masked) {
+      // what stands behind the last visible token, or in no page, is not read as a number
+      const int left = hi - vt;
+      unsigned keep[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int b = left - 4 * q;
+        keep[q] = b >= 4 ? 0xffffffffu : b <= 0 ? 0u : (1u << (8 * b)) - 1u;
+      }
+      unsigned any = 0;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        vr[j].x &= keep[0]; vr[j].y &= keep[1]; vr[j].z &= keep[2]; vr[j].w &= keep[3];
+        if (lo < hi) any |= nan_bytes(vr[j].x) | nan_bytes(vr[j].y) | nan_bytes(vr[j].z) | nan_bytes(vr[j].w);
+      }
+      // A NaN's product is a NaN also with the weight of a column that does not see it.  So it leaves the product, and the columns that do
+      // see one are told by a product of their own: ones where there is a NaN, times ones where a column sees.
+      if (__ballot(any != 0)) {
+        bf16x8 see[NC][2];
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) see[n][half][e] = (bf16_t)(vt + half * 8 + e < lim[n] && pv >= 0 ? 1.f : 0.f);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const unsigned b[4] = {nan_bytes(vr[j].x), nan_bytes(vr[j].y), nan_bytes(vr[j].z), nan_bytes(vr[j].w)};
+          const bf16x8 one0 = codes8(b[0] & 0x38383838u, b[1] & 0x38383838u), one1 = codes8(b[2] & 0x38383838u, b[3] & 0x38383838u);
+          vr[j].x &= ~b[0]; vr[j].y &= ~b[1]; vr[j].z &= ~b[2]; vr[j].w &= ~b[3];
+#pragma unroll
+          for (int n = 0; n < NC; ++n) {
+            f32x4 hits = {0.f, 0.f, 0.f, 0.f};
+            hits = mma(one0, see[n][0], hits);
+            hits = mma(one1, see[n][1], hits);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (hits[r] > 0.f) acc[n][j][r] = __builtin_bit_cast(float, 0x7fc00000u);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      if (j * 16 >= dh) continue;
+      const bf16x8 v0 = codes8(vr[j].x, vr[j].y), v1 = codes8(vr[j].z, vr[j].w);
+#pragma unroll
+      for (int n = 0; n < NC; ++n)
+#pragma unroll
+        for (int q = WP - 1; q >= 0; --q) {
+          acc[n][j] = mma(v0, wf[n][0][q], acc[n][j]);
+          acc[n][j] = mma(v1, wf[n][1][q], acc[n][j]);
+        }
+    }
+  }
+
+  // the four lanes of a column, then the waves, two by two
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    l[n] += __shfl_xor(l[n], 16, 64);
+    l[n] += __shfl_xor(l[n], 32, 64);
+    int any = seen[n];
+    any |= __shfl_xor(any, 16, 64);
+    any |= __shfl_xor(any, 32, 64);
+    if (any && m[n] == -INFINITY && l[n] == 0.f) l[n] = -1.f;
+    for (int step = kWaves / 2; step > 0; step >>= 1) {
+      __syncthreads();
+      if (wave >= step && wave < 2 * step) {
+        if (g == 0) { sml[wave - step][0][i] = m[n]; sml[wave - step][1][i] = l[n]; }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4*>(&so[wave - step][i][j * 16 + g * 4]) = acc[n][j];
+      }
+      __syncthreads();
+      if (wave < step) {
+        const float m2 = sml[wave][0][i], l2 = sml[wave][1][i], top = fmaxf(m[n], m2), base = top == -INFINITY ? 0.f : top;
+        const float f = __builtin_amdgcn_exp2f(m[n] - base), f2 = __builtin_amdgcn_exp2f(m2 - base);
+        if (top == -INFINITY) l[n] = l[n] < 0.f || l2 < 0.f ? -1.f : l[n] + l2;       // nothing but minus infinities (or NaN) so far
+        else l[n] = (l[n] < 0.f ? 0.f : l[n] * f) + (l2 < 0.f ? 0.f : l2 * f2);
+        m[n] = top;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[n][j] = acc[n][j] * f + *reinterpret_cast<const f32x4*>(&so[wave][i][j * 16 + g * 4]) * f2;
+      }
+    }
+    if (wave != 0) continue;
+    const Column col = column_of(s, a, w.h, col0 + n * 16 + i);
+    if (w.pieces > 1) {
+      float* out = a.part + ((int64_t)w.slot * 16 * NC + n * 16 + i) * (dh + 2);
+      if (g == 0) { out[dh] = m[n]; out[dh + 1] = l[n]; }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        if (j * 16 < dh) {
+          *reinterpret_cast<float2*>(out + j * 16 + g * 4) = make_float2(acc[n][j][0], acc[n][j][1]);
+          *reinterpret_cast<float2*>(out + j * 16 + g * 4 + 2) = make_float2(acc[n][j][2], acc[n][j][3]);
+        }
+    } else if (col.there) {
+      const float f = over(m[n], l[n]);
+      T* out = (T*)a.o + col.row * a.ldo + col.head * dh;
+      if (a.lse && g == 0) a.lse[col.row * a.H + col.head] = log_sum(m[n], l[n]);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        if (j * 16 < dh) put4(out + j * 16 + g * 4, acc[n][j] * f, a.vec);
+    }
+  }
+}
+
+// The pieces of a divided axis, in their order.
+template <typename T>
+__global__ void __launch_bounds__(256) k_cache_join(CacheView c, AttnArgs a, int width) {
+  Work w;
+  if (!find_work(c, a, width, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, true, &w) || w.pieces < 2) return;
+  const Sequence s = sequence_of(c, w.b);
+  const int dh = c.dh, quads = dh / 4;
+  for (int it = threadIdx.x; it < width * quads; it += 256) {
+    const int n = it / quads, d = (it - n * quads) * 4;
+    const Column col = column_of(s, a, w.h, w.tile * width + n);
+    if (!col.there) continue;
+    const float* p = a.part + ((int64_t)w.slot * width + n) * (dh + 2);
+    const int64_t step = (int64_t)width * (dh + 2);
+    float top = -INFINITY;
+    for (int i = 0; i < w.pieces; ++i) top = fmaxf(top, p[i * step + dh]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float l = 0.f;
+    bool none = false;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < w.pieces; ++i) {
+      const float* q = p + i * step;
+      const float f = __builtin_amdgcn_exp2f(q[dh] - base), li = q[dh + 1];
+      none |= li < 0.f;
+      l += li < 0.f ? 0.f : top == -INFINITY ? li : li * f;
+      const float2 x = *reinterpret_cast<const float2*>(q + d), y = *reinterpret_cast<const float2*>(q + d + 2);
+      o[0] += x.x * f; o[1] += x.y * f; o[2] += y.x * f; o[3] += y.y * f;
+    }
+    if (none && top == -INFINITY && l == 0.f) l = -1.f;
+    if (a.lse && d == 0) a.lse[col.row * a.H + col.head] = log_sum(top, l);
+    put4((T*)a.o + col.row * a.ldo + col.head * dh + d, o * over(top, l), a.vec);
+  }
+}
+
+// Column tiles of 16 that a block takes side by side, and the pieces that axes are cut into.
+struct Shape { int nc, tiles, target; };
+Shape shape_of(int B, int T, int H, int Hkv, int dh, int64_t tokens) {
+  Shape s;
+  const int64_t columns = (int64_t)T * (H / Hkv);
+  const int most = dh <= 64 ? 4 : dh <= 128 ? 2 : 1;         // that registers hold
+  s.nc = columns <= 16 ? 1 : columns <= 32 ? 2 : 4;
+  if (s.nc > most) s.nc = most;
+  s.tiles = (int)((columns + 16 * s.nc - 1) / (16 * s.nc));
+  const int64_t pairs = (int64_t)B * Hkv * s.tiles, longest = (tokens + 63) / 64;
+  s.target = 1024;
+  // nothing to cut: short axes, or more of them than blocks are wanted
+  if (longest <= 2 * kWaves || pairs >= 4 * s.target || B > 1 << 16) s.target = 0;
+  else if (pairs * ((longest + kWaves - 1) / kWaves) < s.target) s.target = (int)(pairs * ((longest + kWaves - 1) / kWaves));
+  return s;
+}
+
+}  // namespace
+
+bool cache_ok(const CacheView& c, int page);
+bool cache_operands_ok(const CacheView& c);
+
+bool cache_attn_ok(int B, int T, int H, int Hkv, int dh, int page, int max_pages) {
+  CacheView v{};
+  v.B = B; v.T = T; v.Hkv = Hkv; v.dh = dh; v.max_pages = max_pages; v.n_pages = 1; v.rows = 0x7fffffff;
+  return cache_ok(v, page) && H >= Hkv && H % Hkv == 0 && H <= 1 << 16 && (int64_t)T * (H / Hkv) < (int64_t)1 << 30;
+}
+size_t cache_attn_scratch(int B, int T, int H, int Hkv, int dh, int page, int max_pages) {
+  if (!cache_attn_ok(B, T, H, Hkv, dh, page, max_pages)) return 0;
+  const Shape s = shape_of(B, T, H, Hkv, dh, (int64_t)max_pages * page);
+  return (size_t)2 * s.target * 16 * s.nc * (dh + 2);
+}
+
+hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse, int H, int causal) {
+  const int page = 1 << view.shift, dh = view.dh;
+  if (!cache_attn_ok(view.B, view.T, H, view.Hkv, dh, page, view.max_pages)) return hipErrorInvalidValue;
+  const int64_t width = (int64_t)H * dh, widest = (int64_t)1 << 32;
+  if (ldq < width || ldo < width || ldq > widest || ldo > widest) return hipErrorInvalidValue;
+  if (view.B == 0 || view.rows == 0) return hipSuccess;
+  if (!q || !o || !cache_operands_ok(view)) return hipErrorInvalidValue;
+  const Shape s = shape_of(view.B, view.T, H, view.Hkv, dh, (int64_t)view.max_pages * page);
+  const size_t need = cache_attn_scratch(view.B, view.T, H, view.Hkv, dh, page, view.max_pages);
+  if (need && (!c.partial || c.partial_elems < need || ((uintptr_t)c.partial & 7))) return hipErrorInvalidValue;
+  const int G = H / view.Hkv;
+  AttnArgs a{q, o, lse, c.partial, ldq, ldo, H, G, causal != 0, s.tiles, s.target,
+             ldq % 8 == 0 && ldo % 8 == 0 && (((uintptr_t)q | (uintptr_t)o) & 15) == 0, kLog2e / sqrtf((float)dh)};
+  const int64_t pairs = (int64_t)view.B * view.Hkv * s.tiles;
+  auto grid = [](int64_t blocks) {
+    constexpr int64_t most = 1 << 21;            // a launch has less than 2^32 threads along x
+    return dim3((unsigned)(blocks < most ? blocks : most), (unsigned)((blocks + most - 1) / most));
+  };
+  if (pairs > (int64_t)1 << 32) return hipErrorInvalidValue;
+  auto go = [&](auto t, auto nd, auto nc) {
+    typedef decltype(t) T;
+    k_cache_attn<T, decltype(nd)::value, decltype(nc)::value><<<grid(pairs + s.target), 64 * kWaves, 0, c.stream>>>(view, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !s.target) return e;
+    k_cache_join<T><<<grid(pairs), 256, 0, c.stream>>>(view, a, 16 * s.nc);
+    return hipGetLastError();
+  };
+  auto by_columns = [&](auto t, auto nd) {
+    constexpr int ND = decltype(nd)::value;
+    if constexpr (ND == 1) if (s.nc == 4) return go(t, nd, std::integral_constant<int, 4>());
+    if constexpr (ND <= 2) if (s.nc == 2) return go(t, nd, std::integral_constant<int, 2>());
+    return go(t, nd, std::integral_constant<int, 1>());
+  };
+  auto by_head = [&](auto t) {
+    if (dh <= 64) return by_columns(t, std::integral_constant<int, 1>());
+    if (dh <= 128) return by_columns(t, std::integral_constant<int, 2>());
+    if (dh <= 192) return by_columns(t, std::integral_constant<int, 3>());
+    return by_columns(t, std::integral_constant<int, 4>());
+  };
+  return c.dt == BF16 ? by_head(bf16_t()) : by_head(float());
+}
+
+}  // namespace lp

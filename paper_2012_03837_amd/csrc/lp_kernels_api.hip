@@ -3,6 +3,7 @@
 #include <mutex>
 
 #include "../../include/lp_kernels.h"
+#include "cache.h"
 #include "common.h"
 #include "gemm_common.h"
 
@@ -24,6 +25,14 @@ hipError_t attn_bwd_mfma(const OpCtx& c, const void* qkv, const void* o, const f
 hipError_t conv_fwd_plain(const OpCtx& c, const ConvArgs& a, const void* x, const void* w, void* out);
 hipError_t conv_bwd_data_plain(const OpCtx& c, const ConvArgs& a, const void* dout, const void* w, void* dx,
                                const void* add = nullptr);
+hipError_t op_rotary(const OpCtx& c, const void* x, int64_t ldx, void* y, int64_t ldy, const int32_t* pos, const double* freq, int rows,
+                     int S, int heads, int dh, int rot, int interleaved, float scale, int backward);
+bool rotary_frequencies(double* freq, int rot, double base, double factor, double low, double high, double context);
+bool cache_ok(const CacheView& c, int page);
+hipError_t op_cache_append(const OpCtx& c, const CacheView& view, const void* k, int64_t ldk, const void* v, int64_t ldv);
+hipError_t op_cache_read(const OpCtx& c, const CacheView& view, void* k, int64_t ldk, void* v, int64_t ldv);
+size_t cache_attn_scratch(int B, int T, int H, int Hkv, int dh, int page, int max_pages);
+hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse, int H, int causal);
 hipError_t conv_bwd_weight_plain(const OpCtx& c, const ConvArgs& a, const void* dout, const void* x, float* dw,
                                  int accumulate);
 }
@@ -168,6 +177,46 @@ extern "C" int lpk_rmsnorm_bwd(int dtype, const void* dy, const void* r, const f
   return (int)op_rmsnorm_bwd(mk(dtype, stream, scratch, scratch_elems), dy, r, rstd, g, add, dres, dx, dg, rows, d, accumulate, p, rng, site);
 }
 extern "C" size_t lpk_rmsnorm_scratch(int rows, int d) { return rmsnorm_scratch(rows, d); }
+
+extern "C" int lpk_rotary_frequencies(double* freq, int rot, double base, double factor, double low, double high, double context) {
+  return rotary_frequencies(freq, rot, base, factor, low, high, context) ? 0 : (int)hipErrorInvalidValue;
+}
+extern "C" int lpk_rotary(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const int32_t* pos, const double* freq, int rows, int S,
+                          int heads, int dh, int rot, int interleaved, float scale, int backward, void* stream) {
+  if (!dtype_ok(dtype)) return (int)hipErrorInvalidValue;
+  return (int)op_rotary(mk(dtype, stream), x, ldx, y, ldy, pos, freq, rows, S, heads, dh, rot, interleaved, scale, backward);
+}
+static bool mkcache(CacheView* c, int dtype, int rows, const int32_t* starts, const int32_t* lens, const int32_t* table, const void* kpages,
+                    const void* vpages, const float* kscale, const float* vscale, int B, int T, int Hkv, int dh, int page, int max_pages, int n_pages) {
+  *c = CacheView{starts, lens, table, (uint8_t*)kpages, (uint8_t*)vpages, (float*)kscale, (float*)vscale, B, T, rows, Hkv, dh, 0, max_pages, n_pages};
+  while (c->shift < 30 && 1 << c->shift < page) ++c->shift;
+  return dtype_ok(dtype) && cache_ok(*c, page);
+}
+extern "C" int lpk_cache_append(int dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, int rows, const int32_t* starts,
+                                const int32_t* lens, const int32_t* table, void* kpages, void* vpages, float* kscale, float* vscale, int B, int T,
+                                int Hkv, int dh, int page, int max_pages, int n_pages, void* stream) {
+  CacheView c;
+  if (!mkcache(&c, dtype, rows, starts, lens, table, kpages, vpages, kscale, vscale, B, T, Hkv, dh, page, max_pages, n_pages)) return (int)hipErrorInvalidValue;
+  return (int)op_cache_append(mk(dtype, stream), c, k, ldk, v, ldv);
+}
+extern "C" int lpk_cache_read(int dtype, void* k, int64_t ldk, void* v, int64_t ldv, int rows, const int32_t* starts, const int32_t* lens,
+                              const int32_t* table, const void* kpages, const void* vpages, const float* kscale, const float* vscale, int B, int T,
+                              int Hkv, int dh, int page, int max_pages, int n_pages, void* stream) {
+  CacheView c;
+  if (!mkcache(&c, dtype, rows, starts, lens, table, kpages, vpages, kscale, vscale, B, T, Hkv, dh, page, max_pages, n_pages)) return (int)hipErrorInvalidValue;
+  return (int)op_cache_read(mk(dtype, stream), c, k, ldk, v, ldv);
+}
+extern "C" int lpk_cache_attention(int dtype, const void* q, int64_t ldq, int rows, const int32_t* starts, const int32_t* lens, const int32_t* table,
+                                   const void* kpages, const void* vpages, const float* kscale, const float* vscale, void* o, int64_t ldo, float* lse,
+                                   int B, int T, int H, int Hkv, int dh, int page, int max_pages, int n_pages, int causal, float* scratch,
+                                   size_t scratch_elems, void* stream) {
+  CacheView c;
+  if (!mkcache(&c, dtype, rows, starts, lens, table, kpages, vpages, kscale, vscale, B, T, Hkv, dh, page, max_pages, n_pages)) return (int)hipErrorInvalidValue;
+  return (int)op_cache_attn(mk(dtype, stream, scratch, scratch_elems), c, q, ldq, o, ldo, lse, H, causal);
+}
+extern "C" size_t lpk_cache_attention_scratch(int B, int T, int H, int Hkv, int dh, int page, int max_pages) {
+  return cache_attn_scratch(B, T, H, Hkv, dh, page, max_pages);
+}
 
 extern "C" int lpk_layernorm_fwd(int dtype, const void* x, const float* g, const float* b, void* y, float* mean,
                                  float* rstd, int rows, int d, void* stream) {

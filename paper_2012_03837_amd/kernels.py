@@ -106,6 +106,12 @@ _TYPES = {
     "lpk_rmsnorm_fwd": (_i, [_i] + [_vp] * 8 + [_i, _i, _f, _f, _vp, _u32, _vp]),
     "lpk_rmsnorm_bwd": (_i, [_i] + [_vp] * 8 + [_i] * 3 + [_f, _vp, _u32, _vp, _sz, _vp]),
     "lpk_rmsnorm_scratch": (_sz, [_i] * 2),
+    "lpk_rotary": (_i, [_i] + [_vp, _i64] * 2 + [_vp] * 2 + [_i] * 6 + [_f, _i, _vp]),
+    "lpk_rotary_frequencies": (_i, [_vp, _i] + [C.c_double] * 5),
+    "lpk_cache_append": (_i, [_i] + [_vp, _i64] * 2 + [_i] + [_vp] * 7 + [_i] * 7 + [_vp]),
+    "lpk_cache_read": (_i, [_i] + [_vp, _i64] * 2 + [_i] + [_vp] * 7 + [_i] * 7 + [_vp]),
+    "lpk_cache_attention": (_i, [_i, _vp, _i64, _i] + [_vp] * 8 + [_i64, _vp] + [_i] * 9 + [_vp, _sz, _vp]),
+    "lpk_cache_attention_scratch": (_sz, [_i] * 7),
 }
 _entry = {}
 
@@ -125,7 +131,7 @@ def _real(dtype):
     if not _T:
         import torch
         _T.update({0: (torch.float32,), 1: (torch.bfloat16,), "i32": (torch.int32,), "u64": (torch.int64, torch.uint64),
-                   "e4m3": (torch.float8_e4m3fn, torch.uint8), "torch": torch})
+                   "e4m3": (torch.float8_e4m3fn, torch.uint8), "f64": (torch.float64,), "torch": torch})
     if dtype in (0, 1):
         return _T[dtype]
     raise KernelError(f"dtype {dtype!r}: 0 (fp32) or 1 (bf16) is needed")
@@ -225,6 +231,75 @@ def lpk_rmsnorm_bwd(dtype, dy, r, rstd, g, add, dres, dx, dg, rows, d, accumulat
     _run("lpk_rmsnorm_bwd", dev, dtype, _at(dy, e, n, dev), _at(r, e, n, dev), _at(rstd, f, rows, dev), _at(g, f, d, dev), _at(add, e, n, dev),
          _at(dres, e, n, dev), _at(dx, e, n, dev), _at(dg, f, d, dev), rows, d, accumulate, p, _at(rng, _T["u64"], 2, dev),
          site if -1 < site < 1 << 32 else _site(site), _at(scratch, f, 0, dev), _size(scratch))
+
+
+def _mat(t, types, rows, cols, dev):
+    """Address and leading dimension of a matrix of one of the types with so many rows and columns at least, whose rows are contiguous and do not
+    overlap, on the device of that number."""
+    if t is None:
+        return None, cols
+    if t.dtype in types and t.dim() == 2 and t.get_device() == dev:
+        (m, n), (ld, one) = t.shape, t.stride()
+        if m >= rows and n >= cols and (one == 1 or n == 1) and (ld >= n or m < 2):
+            return t.data_ptr(), ld if ld > cols else cols
+    raise KernelError(f"{t.dtype} tensor of {tuple(t.shape)}, strides {t.stride()} on {t.device}: a matrix of at least {rows} rows of {cols} contiguous elements of "
+                      f"{' or '.join(map(str, types))} on the first tensor's device is needed")
+
+
+def lpk_rotary_frequencies(rot, base=10000.0, factor=1.0, low=1.0, high=1.0, context=0.0):
+    """Host tensor of rot / 2 doubles, radians a position; needs no device."""
+    import torch
+    freq = torch.empty(max(0, rot) // 2, dtype=torch.float64)
+    _ck(_fn("lpk_rotary_frequencies")(freq.data_ptr(), rot, base, factor, low, high, context), "lpk_rotary_frequencies")
+    return freq
+
+
+def _wide(n):
+    raise KernelError(f"{n}: a number of 31 bits is needed")
+
+
+def lpk_rotary(dtype, x, y, pos, freq, rows, S, heads, dh, rot, interleaved=0, scale=1.0, backward=0):
+    """x and y: matrices, their rows any distance apart (the q and k columns of qkv, say)."""
+    e, dev = _T.get(dtype) or _real(dtype), _none("lpk_rotary") if x is None else x.get_device()
+    _run("lpk_rotary", dev, dtype, *_mat(x, e, rows, heads * dh, dev), *_mat(y, e, rows, heads * dh, dev), _at(pos, _T["i32"], rows, dev),
+         _at(freq, _T["f64"], rot // 2, dev), rows, S if -1 < S < 1 << 31 else _wide(S), heads, dh, rot, 1 if interleaved else 0, scale, 1 if backward else 0)
+
+
+def _pages(table, kpages, B, Hkv, dh, page):
+    """Page numbers of a sequence in the table, and pages in the pools."""
+    return (0 if table is None else table.numel() // max(1, B)), (0 if kpages is None else kpages.numel() // max(1, Hkv * dh * page))
+
+
+def lpk_cache_append(dtype, k, v, starts, lens, table, kpages, vpages, kscale, vscale, B, T, Hkv, dh, page):
+    """k and v: matrices, their rows any distance apart.  The table has B rows, the pools as many pages as kpages holds."""
+    e, dev = _T.get(dtype) or _real(dtype), _none("lpk_cache_append") if k is None else k.get_device()
+    (most, n), i32, f, q, rows = _pages(table, kpages, B, Hkv, dh, page), _T["i32"], _T[0], _T["e4m3"], k.shape[0]
+    _run("lpk_cache_append", dev, dtype, *_mat(k, e, rows, Hkv * dh, dev), *_mat(v, e, rows, Hkv * dh, dev), rows, _at(starts, i32, B + 1, dev),
+         _at(lens, i32, B, dev), _at(table, i32, B * most, dev), _at(kpages, q, 0, dev), _at(vpages, q, n * Hkv * dh * page, dev), _at(kscale, f, n * Hkv, dev),
+         _at(vscale, f, n * Hkv, dev), B, T if -1 < T < 1 << 31 else _wide(T), Hkv, dh, page, most, n)
+
+
+def lpk_cache_read(dtype, k, v, starts, lens, table, kpages, vpages, kscale, vscale, B, T, Hkv, dh, page):
+    e, dev = _T.get(dtype) or _real(dtype), _none("lpk_cache_read") if k is None else k.get_device()
+    (most, n), i32, f, q, rows = _pages(table, kpages, B, Hkv, dh, page), _T["i32"], _T[0], _T["e4m3"], k.shape[0]
+    _run("lpk_cache_read", dev, dtype, *_mat(k, e, rows, Hkv * dh, dev), *_mat(v, e, rows, Hkv * dh, dev), rows, _at(starts, i32, B + 1, dev),
+         _at(lens, i32, B, dev), _at(table, i32, B * most, dev), _at(kpages, q, 0, dev), _at(vpages, q, n * Hkv * dh * page, dev), _at(kscale, f, n * Hkv, dev),
+         _at(vscale, f, n * Hkv, dev), B, T if -1 < T < 1 << 31 else _wide(T), Hkv, dh, page, most, n)
+
+
+def lpk_cache_attention_scratch(B, T, H, Hkv, dh, page, max_pages):
+    """Floats of workspace; needs no device."""
+    return _fn("lpk_cache_attention_scratch")(B, T, H, Hkv, dh, page, max_pages)
+
+
+def lpk_cache_attention(dtype, q, starts, lens, table, kpages, vpages, kscale, vscale, o, lse, B, T, H, Hkv, dh, page, causal=1, scratch=None):
+    """q and o: matrices, their rows any distance apart."""
+    e, dev = _T.get(dtype) or _real(dtype), _none("lpk_cache_attention") if q is None else q.get_device()
+    (most, n), i32, f, e8, rows = _pages(table, kpages, B, Hkv, dh, page), _T["i32"], _T[0], _T["e4m3"], q.shape[0]
+    _run("lpk_cache_attention", dev, dtype, *_mat(q, e, rows, H * dh, dev), rows, _at(starts, i32, B + 1, dev), _at(lens, i32, B, dev),
+         _at(table, i32, B * most, dev), _at(kpages, e8, 0, dev), _at(vpages, e8, n * Hkv * dh * page, dev), _at(kscale, f, n * Hkv, dev),
+         _at(vscale, f, n * Hkv, dev), *_mat(o, e, rows, H * dh, dev), _at(lse, f, rows * H, dev), B, T if -1 < T < 1 << 31 else _wide(T), H, Hkv, dh, page, most, n, 1 if causal else 0,
+         _at(scratch, f, 0, dev), _size(scratch))
 
 
 def lpk_layernorm_fwd(dtype, x, g, b, y, mean, rstd, rows, d):
