@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "cache.h"
+#include "vec8.h"
 
 namespace lp {
 
@@ -472,6 +473,334 @@ __global__ void __launch_bounds__(64 * kWaves) k_cache_attn(CacheView c, AttnArg
   }
 }
 
+// ------------------------------------------------------------------------------------------------ many rows
+// The same for calls with many columns (prompts, chunks of them): a block has 128 columns or more, a wave 32 or 64 of them, and tiles of 64
+// tokens go through LDS, as numbers, for all its waves: keys in bf16, values in f16, each code converted once.  Products are 32 x 32 x 16; the rows of K are dealt
+// to tokens so that a lane's eight scores, and its operand of the second product, are eight tokens in order (token_of).
+// Weights enter the second product in f16, whose eleven bits leave 2^-12 of a weight (two parts in fp32, 2^-23): codes of 8 bits are f16 numbers too.  f16 has
+// no range to speak of, so that they are held relative to the largest weight times scale of the values that the row has met, which stands at 2^15: weights down
+// to 2^-29 of that have all their bits, less than 2^-40 of it is lost of others.  The sum of weights is of the 32-bit numbers.
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+
+__device__ __forceinline__ f32x16 mma32(const bf16x8& a, const bf16x8& b, const f32x16& c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma32(const f16x8& a, const f16x8& b, const f32x16& c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f16x8 codes8_f16(unsigned a, unsigned b) {
+  const f16x2 p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false), q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true);
+  const f16x2 r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false), s = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true);
+  f16x8 v;
+  v[0] = p[0]; v[1] = p[1]; v[2] = q[0]; v[3] = q[1]; v[4] = r[0]; v[5] = r[1]; v[6] = s[0]; v[7] = s[1];
+  return v;
+}
+// Token of a tile of 32 that row `r` of a product stands for: values 8 kk .. 8 kk + 7 of lane l are rows 16 kk + 4 (l / 32) + {0..3, 8..11}, tokens
+// 16 kk + 8 (l / 32) + {0..7}.
+__device__ __forceinline__ int token_of(int r) { return (r & 16) | (r & 4) << 1 | (r & 8) >> 1 | (r & 3); }
+// The other half's number.
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+// NB: head size in units of 32 columns, rounded up; CG: column groups of 32 of a wave.
+template <typename T, int NB, int CG>
+__global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
+  constexpr bool F = std::is_same<T, float>::value;
+  constexpr int QP = F ? 3 : 1, WP = F ? 2 : 1, DH = 32 * NB, KLD = DH + 8, VLD = 72, kLoads = (64 * (DH / 16) + 255) / 256;
+  constexpr float kTop = 15.f;
+  __shared__ __align__(16) bf16_t sk[2][64][KLD];
+  __shared__ __align__(16) _Float16 sv[2][DH][VLD];
+  __shared__ __align__(8) unsigned short snan[2][DH][4];            // of a tile that not all columns see: which of a column's sixteen tokens are NaN
+  const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const int dh = c.dh, page = 1 << c.shift, width = 128 * CG;
+  Work w;
+  if (a.target) {
+    if (!find_work(c, a, width, id, false, &w)) return;
+  } else {
+    // the longest first, and all column tiles of a head on one of the eight parts of the chip, which share a cache
+    const int pairs = c.B * c.Hkv, stride = (pairs + 7) & ~7, pair = (int)(id % stride);
+    w.tile = a.tiles - 1 - (int)(id / stride);
+    if (pair >= pairs || w.tile < 0) return;
+    w.b = pair / c.Hkv;
+    w.h = pair - w.b * c.Hkv;
+    w.piece = w.slot = 0;
+    w.pieces = 1;
+  }
+  const Sequence s = sequence_of(c, w.b);
+  const int col0 = w.tile * width, columns = s.n * a.G;
+  if (col0 >= columns) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 31, half = lane >> 5, first = col0 + wave * 32 * CG;
+
+  auto limit = [&](int t) {
+    const int v = a.causal ? s.len - s.n + t + 1 : s.len;
+    return v < 0 ? 0 : v;
+  };
+  // visible tokens: of the block's first and last column there is, of the wave's, of the lane's
+  const int blo = limit(col0 / a.G), bhi = limit((col0 + width < columns ? col0 + width - 1 : columns - 1) / a.G);
+  const int lo = limit(first / a.G), hi = first >= columns ? 0 : limit((first + 32 * CG < columns ? first + 32 * CG - 1 : columns - 1) / a.G);
+  int lim[CG];
+  bf16x8 qf[CG][2 * NB][QP];
+#pragma unroll
+  for (int n = 0; n < CG; ++n) {
+    const Column col = column_of(s, a, w.h, first + n * 32 + i);
+    lim[n] = col.there ? limit(col.t) : 0;
+#pragma unroll
+    for (int k = 0; k < 2 * NB; ++k) {
+      const int d = k * 16 + half * 8;
+      float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (col.there && d < dh) {
+        const T* p = (const T*)a.q + col.row * a.ldq + col.head * dh + d;
+        if (a.vec) {
+          load8(p, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = to_f(p[e]);
+        }
+      }
+      split8<QP>(v, qf[n][k]);
+    }
+  }
+  int tile, last;
+  tiles_of((((a.target ? s.len : bhi) + 63) >> 6), w.piece, w.pieces, &tile, &last);
+  if (last > (bhi + 63) >> 6) last = (bhi + 63) >> 6;
+
+  f32x16 acc[CG][NB];
+  float m[CG], top[CG], l[CG];           // largest score; largest score plus the logarithm of its values' scale; sum of weights
+  bool seen[CG];
+#pragma unroll
+  for (int n = 0; n < CG; ++n) {
+    m[n] = top[n] = -INFINITY;
+    l[n] = 0.f;
+    seen[n] = false;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[n][j][v] = 0.f;
+  }
+
+  // A tile on its way: sixteen bytes of a token's keys, and of a column's values, a thread and load.  Of columns behind the head's, of tokens that nobody in the
+  // block sees and of pages that are not there, zeros.
+  uint4 kr[kLoads], vr[kLoads];
+  const int per = dh >> 4;
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int x = tid + 256 * u, tok = x / (DH / 16), d = x % (DH / 16), at = t * 64 + tok;
+      kr[u] = make_uint4(0, 0, 0, 0);
+      if (x < 64 * (DH / 16) && d < per && at < bhi) {
+        const int p = page_of(c, w.b, at >> c.shift);
+        if (p >= 0) kr[u] = *reinterpret_cast<const uint4*>(c.k + ((((int64_t)p * c.Hkv + w.h) << c.shift) + (at & (page - 1))) * dh + d * 16);
+      }
+      const int e = x >> 2, run = t * 64 + (x & 3) * 16;
+      vr[u] = make_uint4(0, 0, 0, 0);
+      if (e < dh && run < bhi) {
+        const int p = page_of(c, w.b, run >> c.shift);
+        if (p >= 0) vr[u] = *reinterpret_cast<const uint4*>(c.v + ((((int64_t)p * c.Hkv + w.h) * dh + e) << c.shift) + (run & (page - 1)));
+      }
+    }
+  };
+  auto stage = [&](int t, int buf) {
+    const bool part = t * 64 + 64 > blo;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int x = tid + 256 * u, tok = x / (DH / 16), d = x % (DH / 16);
+      if (x < 64 * (DH / 16)) {
+        *reinterpret_cast<bf16x8*>(&sk[buf][tok][d * 16]) = codes8(kr[u].x, kr[u].y);
+        *reinterpret_cast<bf16x8*>(&sk[buf][tok][d * 16 + 8]) = codes8(kr[u].z, kr[u].w);
+      }
+      const int e = x >> 2, run = x & 3;
+      if (e < DH) {
+        unsigned q[4] = {vr[u].x, vr[u].y, vr[u].z, vr[u].w};
+        if (part) {
+          // what stands behind the last visible token is no number; a NaN leaves the product, and is told to the columns that see it
+          const int left = bhi - (t * 64 + run * 16);
+          unsigned bits = 0;
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            const int b = left - 4 * z;
+            q[z] &= b >= 4 ? 0xffffffffu : b <= 0 ? 0u : (1u << (8 * b)) - 1u;
+            const unsigned bad = nan_bytes(q[z]);
+            q[z] &= ~bad;
+            bits |= ((bad & 1u) | (bad >> 7 & 2u) | (bad >> 14 & 4u) | (bad >> 21 & 8u)) << (4 * z);
+          }
+          snan[buf][e][run] = (unsigned short)bits;
+        }
+        *reinterpret_cast<f16x8*>(&sv[buf][e][run * 16]) = codes8_f16(q[0], q[1]);
+        *reinterpret_cast<f16x8*>(&sv[buf][e][run * 16 + 8]) = codes8_f16(q[2], q[3]);
+      }
+    }
+  };
+
+  if (tile < last) {
+    fetch(tile);
+    stage(tile, 0);
+  }
+  __syncthreads();
+  for (int t = tile, buf = 0; t < last; ++t, buf ^= 1) {
+    if (t + 1 < last) fetch(t + 1);
+    const int tok = t * 64;
+    if (tok < hi) {
+      const bool masked = tok + 64 > lo;
+      // of the tile's four runs of sixteen tokens: the scales, and whether there is a page
+      float ks[4], vs[4], lv[4];
+      bool here[4], all = true;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int p = tok + r * 16 < bhi ? page_of(c, w.b, (tok + r * 16) >> c.shift) : -1;
+        here[r] = p >= 0;
+        all = all && here[r];
+        const int64_t where = (int64_t)(p < 0 ? 0 : p) * c.Hkv + w.h;
+        ks[r] = here[r] ? c.ks[where] * a.scale : 0.f;
+        vs[r] = here[r] ? c.vs[where] : 0.f;
+        lv[r] = __builtin_amdgcn_logf(vs[r]);
+      }
+      f32x16 sc[CG][2];
+#pragma unroll
+      for (int n = 0; n < CG; ++n)
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) sc[n][g][v] = 0.f;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const bf16_t* kp = &sk[buf][g * 32 + token_of(i)][half * 8];
+#pragma unroll
+        for (int k = 0; k < 2 * NB; ++k) {
+          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + k * 16);
+#pragma unroll
+          for (int n = 0; n < CG; ++n)
+#pragma unroll
+            for (int q = QP - 1; q >= 0; --q) sc[n][g] = mma32(kf, qf[n][k][q], sc[n][g]);
+        }
+      }
+      f16x8 wf[CG][4][WP];
+#pragma unroll
+      for (int n = 0; n < CG; ++n) {
+        float tm = -INFINITY, tt = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          f32x16& x = sc[n][r >> 1];
+          const int v0 = (r & 1) * 8;
+          float best = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float y = x[v0 + e] * ks[r];
+            if (masked || !all) {
+              const bool ok = here[r] && tok + r * 16 + half * 8 + e < lim[n];
+              y = ok ? y : -INFINITY;
+              seen[n] |= ok;
+            }
+            x[v0 + e] = y;
+            best = fmaxf(best, y);
+          }
+          tm = fmaxf(tm, best);
+          tt = fmaxf(tt, best + lv[r]);
+        }
+        if (!masked && all) seen[n] = true;
+        tm = fmaxf(fmaxf(tm, other_half(tm)), m[n]);
+        tt = fmaxf(fmaxf(tt, other_half(tt)), top[n]);
+        const float base = tm == -INFINITY ? 0.f : tm;
+        if (__ballot(tm > m[n] || tt > top[n])) {
+          l[n] *= __builtin_amdgcn_exp2f(m[n] - base);
+          const float f = tt == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top[n] - tt);
+#pragma unroll
+          for (int j = 0; j < NB; ++j) acc[n][j] *= f;
+          m[n] = tm;
+          top[n] = tt;
+        }
+        // at most 2^100: beyond that the weights of the tile are zeros in 32 bits
+        const float lift = tt == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fminf(base - tt, 100.f) + kTop);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float f = vs[r] * lift;
+          float p[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(sc[n][r >> 1][(r & 1) * 8 + e] - base);
+            l[n] += p[e];
+            p[e] *= f;
+          }
+#pragma unroll
+          for (int q = 0; q < WP; ++q)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              wf[n][r][q][e] = (_Float16)p[e];
+              if (q + 1 < WP) p[e] -= (float)wf[n][r][q][e];
+            }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const _Float16* vp = &sv[buf][j * 32 + i][half * 8];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f16x8 vf = *reinterpret_cast<const f16x8*>(vp + r * 16);
+#pragma unroll
+          for (int n = 0; n < CG; ++n)
+#pragma unroll
+            for (int q = WP - 1; q >= 0; --q) acc[n][j] = mma32(vf, wf[n][r][q], acc[n][j]);
+        }
+      }
+      if (tok + 64 > blo) {
+        unsigned long long any = 0;
+        for (int d = lane; d < DH; d += 64) any |= *reinterpret_cast<const unsigned long long*>(snan[buf][d]);
+        if (__ballot(any != 0)) {
+#pragma unroll
+          for (int n = 0; n < CG; ++n) {
+            const int left = lim[n] - tok;
+            unsigned long long see = left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (!here[r]) see &= ~(0xffffull << (16 * r));
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+              for (int v = 0; v < 16; ++v)
+                if (*reinterpret_cast<const unsigned long long*>(snan[buf][j * 32 + 8 * (v / 4) + 4 * half + v % 4]) & see)
+                  acc[n][j][v] = __builtin_bit_cast(float, 0x7fc00000u);
+          }
+        }
+      }
+    }
+    if (t + 1 < last) stage(t + 1, buf ^ 1);
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int n = 0; n < CG; ++n) {
+    l[n] += other_half(l[n]);
+    int any = seen[n];
+    any |= __shfl_xor(any, 32, 64);
+    if (any && m[n] == -INFINITY && l[n] == 0.f) l[n] = -1.f;
+    const int at = first + n * 32 + i;
+    const Column col = column_of(s, a, w.h, at);
+    // from the weights' reference to the scores'
+    const float back = top[n] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[n] - m[n] - kTop);
+    if (w.pieces > 1) {
+      float* out = a.part + ((int64_t)w.slot * width + at - col0) * (dh + 2);
+      if (half == 0) { out[dh] = m[n]; out[dh + 1] = l[n]; }
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4) {
+          const int d = j * 32 + 2 * v + 4 * half;
+          if (d >= dh) continue;
+          *reinterpret_cast<float2*>(out + d) = make_float2(acc[n][j][v] * back, acc[n][j][v + 1] * back);
+          *reinterpret_cast<float2*>(out + d + 2) = make_float2(acc[n][j][v + 2] * back, acc[n][j][v + 3] * back);
+        }
+    } else if (col.there) {
+      const float f = over(m[n], l[n]) * back;
+      T* out = (T*)a.o + col.row * a.ldo + col.head * dh;
+      if (a.lse && half == 0) a.lse[col.row * a.H + col.head] = log_sum(m[n], l[n]);
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4) {
+          const int d = j * 32 + 2 * v + 4 * half;
+          if (d >= dh) continue;
+          put4(out + d, f32x4{acc[n][j][v] * f, acc[n][j][v + 1] * f, acc[n][j][v + 2] * f, acc[n][j][v + 3] * f}, a.vec);
+        }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ divided axes
 // The pieces of a divided axis, in their order.
 template <typename T>
 __global__ void __launch_bounds__(256) k_cache_join(CacheView c, AttnArgs a, int width) {
@@ -505,19 +834,21 @@ __global__ void __launch_bounds__(256) k_cache_join(CacheView c, AttnArgs a, int
   }
 }
 
-// Column tiles of 16 that a block takes side by side, and the pieces that axes are cut into.
-struct Shape { int nc, tiles, target; };
+// The kernel, the columns of a block, and the pieces that axes are cut into.
+struct Shape { bool prompt; int nc, width, tiles, target; };
 Shape shape_of(int B, int T, int H, int Hkv, int dh, int64_t tokens) {
   Shape s;
   const int64_t columns = (int64_t)T * (H / Hkv);
-  const int most = dh <= 64 ? 4 : dh <= 128 ? 2 : 1;         // that registers hold
-  s.nc = columns <= 16 ? 1 : columns <= 32 ? 2 : 4;
+  const int most = dh <= 64 ? 4 : dh <= 128 ? 2 : 1;         // column tiles of 16 that registers hold
+  s.prompt = columns > 64;
+  s.nc = s.prompt ? 1 : columns <= 16 ? 1 : columns <= 32 ? 2 : 4;
   if (s.nc > most) s.nc = most;
-  s.tiles = (int)((columns + 16 * s.nc - 1) / (16 * s.nc));
+  s.width = s.prompt ? 128 * s.nc : 16 * s.nc;
+  s.tiles = (int)((columns + s.width - 1) / s.width);
   const int64_t pairs = (int64_t)B * Hkv * s.tiles, longest = (tokens + 63) / 64;
-  s.target = 1024;
+  s.target = s.prompt ? 512 : 1024;
   // nothing to cut: short axes, or more of them than blocks are wanted
-  if (longest <= 2 * kWaves || pairs >= 4 * s.target || B > 1 << 16) s.target = 0;
+  if (longest <= 2 * kWaves || pairs >= (s.prompt ? s.target : 4 * s.target) || B > 1 << 16) s.target = 0;
   else if (pairs * ((longest + kWaves - 1) / kWaves) < s.target) s.target = (int)(pairs * ((longest + kWaves - 1) / kWaves));
   return s;
 }
@@ -535,7 +866,7 @@ bool cache_attn_ok(int B, int T, int H, int Hkv, int dh, int page, int max_pages
 size_t cache_attn_scratch(int B, int T, int H, int Hkv, int dh, int page, int max_pages) {
   if (!cache_attn_ok(B, T, H, Hkv, dh, page, max_pages)) return 0;
   const Shape s = shape_of(B, T, H, Hkv, dh, (int64_t)max_pages * page);
-  return (size_t)2 * s.target * 16 * s.nc * (dh + 2);
+  return (size_t)2 * s.target * s.width * (dh + 2);
 }
 
 hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse, int H, int causal) {
@@ -556,13 +887,23 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
     constexpr int64_t most = 1 << 21;            // a launch has less than 2^32 threads along x
     return dim3((unsigned)(blocks < most ? blocks : most), (unsigned)((blocks + most - 1) / most));
   };
-  if (pairs > (int64_t)1 << 32) return hipErrorInvalidValue;
+  if (pairs > (int64_t)1 << 32 || (int64_t)view.B * view.Hkv > 1 << 30) return hipErrorInvalidValue;
   auto go = [&](auto t, auto nd, auto nc) {
     typedef decltype(t) T;
     k_cache_attn<T, decltype(nd)::value, decltype(nc)::value><<<grid(pairs + s.target), 64 * kWaves, 0, c.stream>>>(view, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !s.target) return e;
-    k_cache_join<T><<<grid(pairs), 256, 0, c.stream>>>(view, a, 16 * s.nc);
+    k_cache_join<T><<<grid(pairs), 256, 0, c.stream>>>(view, a, s.width);
+    return hipGetLastError();
+  };
+  auto many = [&](auto t, auto nb) {
+    typedef decltype(t) T;
+    constexpr int NB = decltype(nb)::value;
+    const int64_t blocks = s.target ? pairs + s.target : (((int64_t)view.B * view.Hkv + 7) & ~(int64_t)7) * s.tiles;
+    k_cache_prompt<T, NB, 1><<<grid(blocks), 256, 0, c.stream>>>(view, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !s.target) return e;
+    k_cache_join<T><<<grid(pairs), 256, 0, c.stream>>>(view, a, s.width);
     return hipGetLastError();
   };
   auto by_columns = [&](auto t, auto nd) {
@@ -572,6 +913,14 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
     return go(t, nd, std::integral_constant<int, 1>());
   };
   auto by_head = [&](auto t) {
+    if (s.prompt) {
+      if (dh <= 32) return many(t, std::integral_constant<int, 1>());
+      if (dh <= 64) return many(t, std::integral_constant<int, 2>());
+      if (dh <= 96) return many(t, std::integral_constant<int, 3>());
+      if (dh <= 128) return many(t, std::integral_constant<int, 4>());
+      if (dh <= 192) return many(t, std::integral_constant<int, 6>());
+      return many(t, std::integral_constant<int, 8>());
+    }
     if (dh <= 64) return by_columns(t, std::integral_constant<int, 1>());
     if (dh <= 128) return by_columns(t, std::integral_constant<int, 2>());
     if (dh <= 192) return by_columns(t, std::integral_constant<int, 3>());
