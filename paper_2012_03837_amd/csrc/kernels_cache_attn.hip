@@ -478,8 +478,9 @@ __global__ void __launch_bounds__(64 * kWaves) k_cache_attn(CacheView c, AttnArg
 // tokens go through LDS, as numbers, for all its waves: keys in bf16, values in f16, each code converted once.  Products are 32 x 32 x 16; the rows of K are dealt
 // to tokens so that a lane's eight scores, and its operand of the second product, are eight tokens in order (token_of).
 // Weights enter the second product in f16, whose eleven bits leave 2^-12 of a weight (two parts in fp32, 2^-23): codes of 8 bits are f16 numbers too.  f16 has
-// no range to speak of, so that they are held relative to the largest weight times scale of the values that the row has met, which stands at 2^15: weights down
-// to 2^-29 of that have all their bits, less than 2^-40 of it is lost of others.  The sum of weights is of the 32-bit numbers.
+// no range to speak of, so that they are held relative to the largest weight times scale of the values that the row has met (`top`), at 2^7 of which one stands;
+// both it and the largest score lag by a factor of up to 2^8, so that sums are seldom rescaled.  Weights down to 2^-21 of the largest have all their bits, 2^-32 of it is
+// lost of others.  One exponential gives a weight with its values' scale; the sum of weights takes the scale out again, run by run, and is of 32-bit numbers.
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 
@@ -495,18 +496,27 @@ __device__ __forceinline__ f16x8 codes8_f16(unsigned a, unsigned b) {
 // Token of a tile of 32 that row `r` of a product stands for: values 8 kk .. 8 kk + 7 of lane l are rows 16 kk + 4 (l / 32) + {0..3, 8..11}, tokens
 // 16 kk + 8 (l / 32) + {0..7}.
 __device__ __forceinline__ int token_of(int r) { return (r & 16) | (r & 4) << 1 | (r & 8) >> 1 | (r & 3); }
-// The other half's number.
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+// The larger of the two halves' numbers.  (The exchange's results are copied first: a bit cast straight from a vector's element takes the first one.)
+__device__ __forceinline__ float both_max(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const unsigned x = r[0], y = r[1];
+  return fmaxf(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y));
+}
+
+constexpr int kRuns = 128;                 // of sixteen tokens, whose pages and scales are known to a block ahead of their tiles
+struct Runs { int page[kRuns]; float ks[kRuns], lv[kRuns], rv[kRuns]; };
 
 // NB: head size in units of 32 columns, rounded up; CG: column groups of 32 of a wave.
 template <typename T, int NB, int CG>
 __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
   constexpr bool F = std::is_same<T, float>::value;
   constexpr int QP = F ? 3 : 1, WP = F ? 2 : 1, DH = 32 * NB, KLD = DH + 8, VLD = 72, kLoads = (64 * (DH / 16) + 255) / 256;
-  constexpr float kTop = 15.f;
+  constexpr float kTop = 7.f, kLag = 8.f;
   __shared__ __align__(16) bf16_t sk[2][64][KLD];
   __shared__ __align__(16) _Float16 sv[2][DH][VLD];
-  __shared__ __align__(8) unsigned short snan[2][DH][4];            // of a tile that not all columns see: which of a column's sixteen tokens are NaN
+  __shared__ __align__(16) Runs runs[2];
+  __shared__ __align__(8) unsigned short snan[2][DH][4];     // of a tile that not all columns see: which of a column's sixteen tokens are NaN
   const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   const int dh = c.dh, page = 1 << c.shift, width = 128 * CG;
   Work w;
@@ -525,7 +535,7 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
   const Sequence s = sequence_of(c, w.b);
   const int col0 = w.tile * width, columns = s.n * a.G;
   if (col0 >= columns) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 31, half = lane >> 5, first = col0 + wave * 32 * CG;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 31, half = lane >> 5, first = col0 + wave * 32 * CG;
 
   auto limit = [&](int t) {
     const int v = a.causal ? s.len - s.n + t + 1 : s.len;
@@ -534,6 +544,25 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
   // visible tokens: of the block's first and last column there is, of the wave's, of the lane's
   const int blo = limit(col0 / a.G), bhi = limit((col0 + width < columns ? col0 + width - 1 : columns - 1) / a.G);
   const int lo = limit(first / a.G), hi = first >= columns ? 0 : limit((first + 32 * CG < columns ? first + 32 * CG - 1 : columns - 1) / a.G);
+  int tile, last;
+  tiles_of((((a.target ? s.len : bhi) + 63) >> 6), w.piece, w.pieces, &tile, &last);
+  if (last > (bhi + 63) >> 6) last = (bhi + 63) >> 6;
+
+  // 32 tiles' runs from tile t on; the two sets take turns
+  auto known = [&](int t) -> Runs& { return runs[(t - tile) >> 5 & 1]; };
+  auto look_up = [&](int t) {
+    if (tid >= kRuns) return;
+    const int at = t * 64 + tid * 16, p = at < bhi ? page_of(c, w.b, at >> c.shift) : -1;
+    const int64_t where = (int64_t)(p < 0 ? 0 : p) * c.Hkv + w.h;
+    const float vs = p < 0 ? 1.f : c.vs[where];
+    Runs& r = known(t);
+    r.page[tid] = p;
+    r.ks[tid] = p < 0 ? 1.f : c.ks[where] * a.scale;
+    r.lv[tid] = __builtin_amdgcn_logf(vs);
+    r.rv[tid] = 1.f / vs;
+  };
+  if (tile < last) look_up(tile);
+
   int lim[CG];
   bf16x8 qf[CG][2 * NB][QP];
 #pragma unroll
@@ -556,9 +585,6 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
       split8<QP>(v, qf[n][k]);
     }
   }
-  int tile, last;
-  tiles_of((((a.target ? s.len : bhi) + 63) >> 6), w.piece, w.pieces, &tile, &last);
-  if (last > (bhi + 63) >> 6) last = (bhi + 63) >> 6;
 
   f32x16 acc[CG][NB];
   float m[CG], top[CG], l[CG];           // largest score; largest score plus the logarithm of its values' scale; sum of weights
@@ -578,20 +604,23 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
   // block sees and of pages that are not there, zeros.
   uint4 kr[kLoads], vr[kLoads];
   const int per = dh >> 4;
+  const int64_t page_bytes = (int64_t)c.Hkv * dh << c.shift;
+  const uint8_t *kh = c.k + ((int64_t)w.h * dh << c.shift), *vh = c.v + ((int64_t)w.h * dh << c.shift);
   auto fetch = [&](int t) {
+    const Runs& r = known(t);
+    const int run0 = (t - tile & 31) * 4;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
-      const int x = tid + 256 * u, tok = x / (DH / 16), d = x % (DH / 16), at = t * 64 + tok;
-      kr[u] = make_uint4(0, 0, 0, 0);
-      if (x < 64 * (DH / 16) && d < per && at < bhi) {
-        const int p = page_of(c, w.b, at >> c.shift);
-        if (p >= 0) kr[u] = *reinterpret_cast<const uint4*>(c.k + ((((int64_t)p * c.Hkv + w.h) << c.shift) + (at & (page - 1))) * dh + d * 16);
+      const int x = tid + 256 * u, tok = x / (DH / 16), d = x % (DH / 16);
+      kr[u] = vr[u] = make_uint4(0, 0, 0, 0);
+      if (x < 64 * (DH / 16) && d < per) {
+        const int p = r.page[run0 + (tok >> 4)];
+        if (p >= 0) kr[u] = *reinterpret_cast<const uint4*>(kh + p * page_bytes + ((t * 64 + tok) & (page - 1)) * dh + d * 16);
       }
-      const int e = x >> 2, run = t * 64 + (x & 3) * 16;
-      vr[u] = make_uint4(0, 0, 0, 0);
-      if (e < dh && run < bhi) {
-        const int p = page_of(c, w.b, run >> c.shift);
-        if (p >= 0) vr[u] = *reinterpret_cast<const uint4*>(c.v + ((((int64_t)p * c.Hkv + w.h) * dh + e) << c.shift) + (run & (page - 1)));
+      const int e = x >> 2;
+      if (e < dh) {
+        const int p = r.page[run0 + (x & 3)];
+        if (p >= 0) vr[u] = *reinterpret_cast<const uint4*>(vh + p * page_bytes + (e << c.shift) + ((t * 64 + (x & 3) * 16) & (page - 1)));
       }
     }
   };
@@ -627,29 +656,28 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
     }
   };
 
+  __syncthreads();
   if (tile < last) {
     fetch(tile);
     stage(tile, 0);
   }
   __syncthreads();
   for (int t = tile, buf = 0; t < last; ++t, buf ^= 1) {
-    if (t + 1 < last) fetch(t + 1);
+    if (t + 1 < last) {
+      if ((t + 1 - tile & 31) == 0) {
+        look_up(t + 1);
+        __syncthreads();
+      }
+      fetch(t + 1);
+    }
     const int tok = t * 64;
     if (tok < hi) {
-      const bool masked = tok + 64 > lo;
-      // of the tile's four runs of sixteen tokens: the scales, and whether there is a page
-      float ks[4], vs[4], lv[4];
-      bool here[4], all = true;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int p = tok + r * 16 < bhi ? page_of(c, w.b, (tok + r * 16) >> c.shift) : -1;
-        here[r] = p >= 0;
-        all = all && here[r];
-        const int64_t where = (int64_t)(p < 0 ? 0 : p) * c.Hkv + w.h;
-        ks[r] = here[r] ? c.ks[where] * a.scale : 0.f;
-        vs[r] = here[r] ? c.vs[where] : 0.f;
-        lv[r] = __builtin_amdgcn_logf(vs[r]);
-      }
+      const Runs& kn = known(t);
+      const int run0 = (t - tile & 31) * 4;
+      const f32x4 ks = *reinterpret_cast<const f32x4*>(&kn.ks[run0]), lv = *reinterpret_cast<const f32x4*>(&kn.lv[run0]),
+                  rv = *reinterpret_cast<const f32x4*>(&kn.rv[run0]);
+      const int4 pg = *reinterpret_cast<const int4*>(&kn.page[run0]);
+      const bool masked = tok + 64 > lo || (pg.x | pg.y | pg.z | pg.w) < 0;
       f32x16 sc[CG][2];
 #pragma unroll
       for (int n = 0; n < CG; ++n)
@@ -672,49 +700,59 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
       f16x8 wf[CG][4][WP];
 #pragma unroll
       for (int n = 0; n < CG; ++n) {
+        if (masked) {
+          const int pages[4] = {pg.x, pg.y, pg.z, pg.w};
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const bool ok = pages[r] >= 0 && tok + r * 16 + half * 8 + e < lim[n];
+              sc[n][r >> 1][(r & 1) * 8 + e] = ok ? sc[n][r >> 1][(r & 1) * 8 + e] : -INFINITY;
+              seen[n] |= ok;
+            }
+        } else {
+          seen[n] = true;
+        }
         float tm = -INFINITY, tt = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          f32x16& x = sc[n][r >> 1];
-          const int v0 = (r & 1) * 8;
-          float best = -INFINITY;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float y = x[v0 + e] * ks[r];
-            if (masked || !all) {
-              const bool ok = here[r] && tok + r * 16 + half * 8 + e < lim[n];
-              y = ok ? y : -INFINITY;
-              seen[n] |= ok;
-            }
-            x[v0 + e] = y;
-            best = fmaxf(best, y);
-          }
+          const f32x16& x = sc[n][r >> 1];
+          const int v = (r & 1) * 8;
+          const float best = fmaxf(fmaxf(fmaxf(fmaxf(x[v], x[v + 1]), x[v + 2]), fmaxf(fmaxf(x[v + 3], x[v + 4]), x[v + 5])), fmaxf(x[v + 6], x[v + 7])) * ks[r];
           tm = fmaxf(tm, best);
           tt = fmaxf(tt, best + lv[r]);
         }
-        if (!masked && all) seen[n] = true;
-        tm = fmaxf(fmaxf(tm, other_half(tm)), m[n]);
-        tt = fmaxf(fmaxf(tt, other_half(tt)), top[n]);
-        const float base = tm == -INFINITY ? 0.f : tm;
-        if (__ballot(tm > m[n] || tt > top[n])) {
-          l[n] *= __builtin_amdgcn_exp2f(m[n] - base);
-          const float f = tt == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top[n] - tt);
+        tm = both_max(tm);
+        tt = both_max(tt);
+        if (__ballot(tm > m[n] + kLag || tt > top[n] + kLag)) {
+          const float mn = fmaxf(m[n], tm), tn = fmaxf(top[n], tt);
+          l[n] *= mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - mn);
+          const float f = tn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top[n] - tn);
 #pragma unroll
           for (int j = 0; j < NB; ++j) acc[n][j] *= f;
-          m[n] = tm;
-          top[n] = tt;
+          m[n] = mn;
+          top[n] = tn;
         }
-        // at most 2^100: beyond that the weights of the tile are zeros in 32 bits
-        const float lift = tt == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fminf(base - tt, 100.f) + kTop);
+        const float base = m[n] == -INFINITY ? 0.f : m[n], off = kTop - (top[n] == -INFINITY ? 0.f : top[n]);
+        // the exponent by which a weight with its values' scale is apart from the weight: where it is so low that weights of some
+        // account would be lost, they take an exponential of their own
+        const float apart = off + base, least = fminf(fminf(lv[0], lv[1]), fminf(lv[2], lv[3])) + apart;
+        const bool lost = __ballot(least < -100.f) != 0;
+        const float back = __builtin_amdgcn_exp2f(-apart);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float f = vs[r] * lift;
-          float p[8];
+          const float up = lv[r] + off;
+          float p[8], sum = 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(sc[n][r >> 1][(r & 1) * 8 + e] - base);
-            l[n] += p[e];
-            p[e] *= f;
+            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][r >> 1][(r & 1) * 8 + e], ks[r], up));
+            sum += p[e];
+          }
+          if (lost) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) l[n] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][r >> 1][(r & 1) * 8 + e], ks[r], -base));
+          } else {
+            l[n] = __builtin_fmaf(sum, back * rv[r], l[n]);
           }
 #pragma unroll
           for (int q = 0; q < WP; ++q)
@@ -743,11 +781,8 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
         if (__ballot(any != 0)) {
 #pragma unroll
           for (int n = 0; n < CG; ++n) {
-            const int left = lim[n] - tok;
-            unsigned long long see = left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (!here[r]) see &= ~(0xffffull << (16 * r));
+            const int left = lim[n] - tok;                     // bits of pages that are not there are zeros
+            const unsigned long long see = left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1;
 #pragma unroll
             for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -764,7 +799,7 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
 
 #pragma unroll
   for (int n = 0; n < CG; ++n) {
-    l[n] += other_half(l[n]);
+    l[n] += __shfl_xor(l[n], 32, 64);
     int any = seen[n];
     any |= __shfl_xor(any, 32, 64);
     if (any && m[n] == -INFINITY && l[n] == 0.f) l[n] = -1.f;
@@ -876,10 +911,13 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
   if (ldq < width || ldo < width || ldq > widest || ldo > widest) return hipErrorInvalidValue;
   if (view.B == 0 || view.rows == 0) return hipSuccess;
   if (!q || !o || !cache_operands_ok(view)) return hipErrorInvalidValue;
-  const Shape s = shape_of(view.B, view.T, H, view.Hkv, dh, (int64_t)view.max_pages * page);
+  Shape s = shape_of(view.B, view.T, H, view.Hkv, dh, (int64_t)view.max_pages * page);
   const size_t need = cache_attn_scratch(view.B, view.T, H, view.Hkv, dh, page, view.max_pages);
   if (need && (!c.partial || c.partial_elems < need || ((uintptr_t)c.partial & 7))) return hipErrorInvalidValue;
   const int G = H / view.Hkv;
+  // 64 columns a wave
+  const bool wide = s.prompt && !s.target && c.dt == BF16 && dh <= 64;
+  if (wide) s.tiles = (int)(((int64_t)view.T * G + 255) / 256);
   AttnArgs a{q, o, lse, c.partial, ldq, ldo, H, G, causal != 0, s.tiles, s.target,
              ldq % 8 == 0 && ldo % 8 == 0 && (((uintptr_t)q | (uintptr_t)o) & 15) == 0, kLog2e / sqrtf((float)dh)};
   const int64_t pairs = (int64_t)view.B * view.Hkv * s.tiles;
@@ -898,9 +936,10 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
   };
   auto many = [&](auto t, auto nb) {
     typedef decltype(t) T;
-    constexpr int NB = decltype(nb)::value;
+    constexpr int NB = decltype(nb)::value, most = NB <= 2 && std::is_same<T, bf16_t>::value ? 2 : 1;
     const int64_t blocks = s.target ? pairs + s.target : (((int64_t)view.B * view.Hkv + 7) & ~(int64_t)7) * s.tiles;
-    k_cache_prompt<T, NB, 1><<<grid(blocks), 256, 0, c.stream>>>(view, a);
+    if (wide) k_cache_prompt<T, NB, most><<<grid(blocks), 256, 0, c.stream>>>(view, a);
+    else k_cache_prompt<T, NB, 1><<<grid(blocks), 256, 0, c.stream>>>(view, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !s.target) return e;
     k_cache_join<T><<<grid(pairs), 256, 0, c.stream>>>(view, a, s.width);
