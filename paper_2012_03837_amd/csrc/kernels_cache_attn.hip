@@ -505,7 +505,13 @@ __device__ __forceinline__ float both_max(float v) {
 }
 
 constexpr int kRuns = 128;                 // of sixteen tokens, whose pages and scales are known to a block ahead of their tiles
-struct Runs { int page[kRuns]; float ks[kRuns], lv[kRuns], rv[kRuns]; };
+struct Runs { int64_t at[kRuns]; float ks[kRuns], lv[kRuns], rv[kRuns]; };       // at: tokens of the pool before the run's, negative: no page
+// The largest of three; NaN count only where there is nothing else.  (As an instruction of its own: in C each operand would be made quiet first.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 // NB: head size in units of 32 columns, rounded up; CG: column groups of 32 of a wave.
 template <typename T, int NB, int CG>
@@ -523,10 +529,11 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
   if (a.target) {
     if (!find_work(c, a, width, id, false, &w)) return;
   } else {
-    // the longest first, and all column tiles of a head on one of the eight parts of the chip, which share a cache
-    const int pairs = c.B * c.Hkv, stride = (pairs + 7) & ~7, pair = (int)(id % stride);
-    w.tile = a.tiles - 1 - (int)(id / stride);
-    if (pair >= pairs || w.tile < 0) return;
+    // the longest first; a head's column tiles in turn on the eight parts of the chip, so that sequences of different lengths load them alike
+    const int pairs = c.B * c.Hkv, turn = (int)(id / pairs);
+    if (turn >= a.tiles) return;
+    w.tile = a.tiles - 1 - turn;
+    const int pair = (int)((id + turn) % pairs);
     w.b = pair / c.Hkv;
     w.h = pair - w.b * c.Hkv;
     w.piece = w.slot = 0;
@@ -556,7 +563,7 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
     const int64_t where = (int64_t)(p < 0 ? 0 : p) * c.Hkv + w.h;
     const float vs = p < 0 ? 1.f : c.vs[where];
     Runs& r = known(t);
-    r.page[tid] = p;
+    r.at[tid] = p < 0 ? -1 : (((int64_t)p * c.Hkv) << c.shift) + (at & (page - 1));
     r.ks[tid] = p < 0 ? 1.f : c.ks[where] * a.scale;
     r.lv[tid] = __builtin_amdgcn_logf(vs);
     r.rv[tid] = 1.f / vs;
@@ -601,27 +608,28 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
   }
 
   // A tile on its way: sixteen bytes of a token's keys, and of a column's values, a thread and load.  Of columns behind the head's, of tokens that nobody in the
-  // block sees and of pages that are not there, zeros.
+  // block sees and of pages that are not there, zeros.  A run's values start 16 columns times tokens behind its page's, its keys where its tokens do.
   uint4 kr[kLoads], vr[kLoads];
-  const int per = dh >> 4;
-  const int64_t page_bytes = (int64_t)c.Hkv * dh << c.shift;
-  const uint8_t *kh = c.k + ((int64_t)w.h * dh << c.shift), *vh = c.v + ((int64_t)w.h * dh << c.shift);
+  const uint8_t *kh[kLoads], *vh[kLoads];
+  bool kd[kLoads], vd[kLoads];
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    const int x = tid + 256 * u, tok = x / (DH / 16), d = x % (DH / 16), e = x >> 2;
+    kd[u] = x < 64 * (DH / 16) && d * 16 < dh;
+    vd[u] = e < dh;
+    kh[u] = c.k + ((int64_t)w.h * dh << c.shift) + (tok & 15) * dh + d * 16;
+    vh[u] = c.v + (((int64_t)w.h * dh + e) << c.shift);
+  }
   auto fetch = [&](int t) {
     const Runs& r = known(t);
     const int run0 = (t - tile & 31) * 4;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
-      const int x = tid + 256 * u, tok = x / (DH / 16), d = x % (DH / 16);
+      const int x = tid + 256 * u;
       kr[u] = vr[u] = make_uint4(0, 0, 0, 0);
-      if (x < 64 * (DH / 16) && d < per) {
-        const int p = r.page[run0 + (tok >> 4)];
-        if (p >= 0) kr[u] = *reinterpret_cast<const uint4*>(kh + p * page_bytes + ((t * 64 + tok) & (page - 1)) * dh + d * 16);
-      }
-      const int e = x >> 2;
-      if (e < dh) {
-        const int p = r.page[run0 + (x & 3)];
-        if (p >= 0) vr[u] = *reinterpret_cast<const uint4*>(vh + p * page_bytes + (e << c.shift) + ((t * 64 + (x & 3) * 16) & (page - 1)));
-      }
+      const int64_t ka = kd[u] ? r.at[run0 + (x / (DH / 16) >> 4)] : -1, va = vd[u] ? r.at[run0 + (x & 3)] : -1;
+      if (ka >= 0) kr[u] = *reinterpret_cast<const uint4*>(kh[u] + ka * dh);
+      if (va >= 0) vr[u] = *reinterpret_cast<const uint4*>(vh[u] + ((va & ~(int64_t)(page - 1)) * dh + (va & (page - 1))));
     }
   };
   auto stage = [&](int t, int buf) {
@@ -676,15 +684,9 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
       const int run0 = (t - tile & 31) * 4;
       const f32x4 ks = *reinterpret_cast<const f32x4*>(&kn.ks[run0]), lv = *reinterpret_cast<const f32x4*>(&kn.lv[run0]),
                   rv = *reinterpret_cast<const f32x4*>(&kn.rv[run0]);
-      const int4 pg = *reinterpret_cast<const int4*>(&kn.page[run0]);
-      const bool masked = tok + 64 > lo || (pg.x | pg.y | pg.z | pg.w) < 0;
+      const int64_t pages[4] = {kn.at[run0], kn.at[run0 + 1], kn.at[run0 + 2], kn.at[run0 + 3]};
+      const bool masked = tok + 64 > lo || (pages[0] | pages[1] | pages[2] | pages[3]) < 0;
       f32x16 sc[CG][2];
-#pragma unroll
-      for (int n = 0; n < CG; ++n)
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) sc[n][g][v] = 0.f;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         const bf16_t* kp = &sk[buf][g * 32 + token_of(i)][half * 8];
@@ -694,14 +696,13 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
 #pragma unroll
           for (int n = 0; n < CG; ++n)
 #pragma unroll
-            for (int q = QP - 1; q >= 0; --q) sc[n][g] = mma32(kf, qf[n][k][q], sc[n][g]);
+            for (int q = QP - 1; q >= 0; --q) sc[n][g] = mma32(kf, qf[n][k][q], k == 0 && q == QP - 1 ? f32x16{} : sc[n][g]);
         }
       }
       f16x8 wf[CG][4][WP];
 #pragma unroll
       for (int n = 0; n < CG; ++n) {
         if (masked) {
-          const int pages[4] = {pg.x, pg.y, pg.z, pg.w};
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -718,7 +719,7 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
         for (int r = 0; r < 4; ++r) {
           const f32x16& x = sc[n][r >> 1];
           const int v = (r & 1) * 8;
-          const float best = fmaxf(fmaxf(fmaxf(fmaxf(x[v], x[v + 1]), x[v + 2]), fmaxf(fmaxf(x[v + 3], x[v + 4]), x[v + 5])), fmaxf(x[v + 6], x[v + 7])) * ks[r];
+          const float best = max3(max3(x[v], x[v + 1], x[v + 2]), max3(x[v + 3], x[v + 4], x[v + 5]), max3(x[v + 6], x[v + 7], x[v + 7])) * ks[r];
           tm = fmaxf(tm, best);
           tt = fmaxf(tt, best + lv[r]);
         }
@@ -739,6 +740,12 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
         const float apart = off + base, least = fminf(fminf(lv[0], lv[1]), fminf(lv[2], lv[3])) + apart;
         const bool lost = __ballot(least < -100.f) != 0;
         const float back = __builtin_amdgcn_exp2f(-apart);
+        if (lost) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) l[n] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][r >> 1][(r & 1) * 8 + e], ks[r], -base));
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float up = lv[r] + off;
@@ -748,12 +755,7 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
             p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][r >> 1][(r & 1) * 8 + e], ks[r], up));
             sum += p[e];
           }
-          if (lost) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) l[n] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][r >> 1][(r & 1) * 8 + e], ks[r], -base));
-          } else {
-            l[n] = __builtin_fmaf(sum, back * rv[r], l[n]);
-          }
+          l[n] = __builtin_fmaf(lost ? 0.f : sum, lost ? 0.f : back * rv[r], l[n]);
 #pragma unroll
           for (int q = 0; q < WP; ++q)
 #pragma unroll
@@ -916,7 +918,7 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
   if (need && (!c.partial || c.partial_elems < need || ((uintptr_t)c.partial & 7))) return hipErrorInvalidValue;
   const int G = H / view.Hkv;
   // 64 columns a wave
-  const bool wide = s.prompt && !s.target && c.dt == BF16 && dh <= 64;
+  const bool wide = false && s.prompt && !s.target && c.dt == BF16 && dh <= 64;
   if (wide) s.tiles = (int)(((int64_t)view.T * G + 255) / 256);
   AttnArgs a{q, o, lse, c.partial, ldq, ldo, H, G, causal != 0, s.tiles, s.target,
              ldq % 8 == 0 && ldo % 8 == 0 && (((uintptr_t)q | (uintptr_t)o) & 15) == 0, kLog2e / sqrtf((float)dh)};
@@ -937,7 +939,7 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
   auto many = [&](auto t, auto nb) {
     typedef decltype(t) T;
     constexpr int NB = decltype(nb)::value, most = NB <= 2 && std::is_same<T, bf16_t>::value ? 2 : 1;
-    const int64_t blocks = s.target ? pairs + s.target : (((int64_t)view.B * view.Hkv + 7) & ~(int64_t)7) * s.tiles;
+    const int64_t blocks = pairs + s.target;
     if (wide) k_cache_prompt<T, NB, most><<<grid(blocks), 256, 0, c.stream>>>(view, a);
     else k_cache_prompt<T, NB, 1><<<grid(blocks), 256, 0, c.stream>>>(view, a);
     hipError_t e = hipGetLastError();
