@@ -21,7 +21,7 @@ namespace lp {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kWaves = 4;                                  // of a block, each with every fourth tile of 64 tokens
+constexpr int kWaves = 4;                                  // of a block where axes are divided
 
 struct AttnArgs {
   const void* q;
@@ -67,98 +67,65 @@ __device__ __forceinline__ unsigned nan_bytes(unsigned w) {
 // What a block works on.
 struct Work { int b, h, tile, piece, pieces, slot; };
 
-// Sum over the block's threads of two numbers, and of those before the thread's own.
-struct Two { unsigned long long a, b; };
-__device__ __forceinline__ Two scan(Two v, Two* before, Two* sh) {
-  Two run = v;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned long long a = __shfl_up(run.a, o, 64), b = __shfl_up(run.b, o, 64);
-    if (lane >= o) { run.a += a; run.b += b; }
-  }
-  __syncthreads();
-  if (lane == 63) sh[wave] = run;
-  __syncthreads();
-  Two base = {0, 0}, all = {0, 0};
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) { base.a += sh[w].a; base.b += sh[w].b; }
-    all.a += sh[w].a;
-    all.b += sh[w].b;
-  }
-  if (before) *before = Two{base.a + run.a - v.a, base.b + run.b - v.b};
-  return all;
-}
-
-// The axes are cut so that all pieces have the same number of tiles, whatever the sequences' lengths: `each` tiles a piece, as
-// many as leave about `target` pieces in all.  Pieces are numbered through sequences, heads, column tiles and the axis; the block finds
-// number `id` (or, by pair, the first piece of pair `id` of (sequence, head, column tile)).  slot: place of the result among those of divided axes, at
-// most 2 target of them.
-__device__ __forceinline__ bool find_work(const CacheView& c, const AttnArgs& a, int width, int64_t id, bool by_pair, Work* w) {
-  if (a.target == 0 || by_pair) {
-    const int64_t rest = id / a.tiles;
-    w->tile = (int)(id % a.tiles);
-    w->h = (int)(rest % c.Hkv);
-    w->b = (int)(rest / c.Hkv);
-    w->piece = w->slot = 0;
-    w->pieces = 1;
-    if (w->b >= c.B) return false;
-    if (a.target == 0) return true;
-  }
-  __shared__ Two sh[kWaves];
-  __shared__ Work found;
-  const int each_thread = (c.B + 255) / 256, from = threadIdx.x * each_thread, to = from + each_thread < c.B ? from + each_thread : c.B;
-  auto size_of = [&](int b, int* tiles) {                    // of a head: column tiles, and tiles of the axis
+// The axes are cut so that all pieces have the same number of tiles, whatever the sequences' lengths: as many as leave about `target` pieces in
+// all.  Pieces are numbered through sequences, heads, column tiles and the axis; this finds piece `id`, alike in every wave and without a barrier.  The host has
+// seen to it that the sums fit 32 bits.
+__device__ __forceinline__ bool find_work(const CacheView& c, const AttnArgs& a, int width, unsigned id, Work* w) {
+  const unsigned number = id;
+  const int lane = threadIdx.x & 63;
+  auto size_of = [&](int b, unsigned* tiles) {               // of a head: column tiles, and tiles of the axis
     const Sequence s = sequence_of(c, b);
-    *tiles = (s.len + 63) >> 6;
-    return (int)(((int64_t)s.n * a.G + width - 1) / width);
+    *tiles = (unsigned)(s.len + 63) >> 6;
+    return ((unsigned)s.n * a.G + width - 1) / width;
   };
-  Two sum = {0, 0};
-  for (int b = from; b < to; ++b) {
-    int tiles;
-    const int columns = size_of(b, &tiles);
-    sum.a += (unsigned long long)columns * tiles;
+  unsigned all = 0, tiles = 0;
+  for (int b = lane; b < c.B; b += 64) {
+    const unsigned columns = size_of(b, &tiles);
+    all += columns * tiles;
   }
-  const unsigned long long all = scan(sum, nullptr, sh).a * c.Hkv;
-  unsigned long long each = (all + a.target - 1) / a.target;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o, 64);
+  all = __builtin_amdgcn_readfirstlane(all) * c.Hkv;
+  unsigned each = (all + a.target - 1) / a.target;
   if (each < kWaves) each = kWaves;
-  sum = Two{0, 0};
-  auto pieces_of = [&](int tiles) { return tiles > 0 ? (int)((tiles + each - 1) / each) : 1; };
-  for (int b = from; b < to; ++b) {
-    int tiles;
-    const unsigned long long pairs = (unsigned long long)size_of(b, &tiles) * c.Hkv;
-    const int pieces = pieces_of(tiles);
-    sum.a += pairs * pieces;
-    sum.b += pieces > 1 ? pairs * pieces : 0;
-  }
-  Two at;
-  const Two total = scan(sum, &at, sh);
-  if (!by_pair && (unsigned long long)id >= total.a) return false;
-  for (int b = from; b < to; ++b) {
-    int tiles;
-    const int columns = size_of(b, &tiles), pieces = pieces_of(tiles);
-    const unsigned long long n = (unsigned long long)columns * c.Hkv * pieces;
-    const bool mine = by_pair ? b == w->b : (unsigned long long)id >= at.a && (unsigned long long)id < at.a + n;
-    if (mine) {
-      const unsigned long long i = by_pair ? ((unsigned long long)w->h * columns + w->tile) * pieces : id - at.a;
-      found.b = b;
-      found.piece = (int)(i % pieces);
-      found.tile = columns ? (int)(i / pieces % columns) : 0;
-      found.h = columns ? (int)(i / pieces / columns) : 0;
-      found.pieces = by_pair && w->tile >= columns ? 1 : pieces;
-      found.slot = (int)(at.b + i);
+  for (int b0 = 0; b0 < c.B; b0 += 64) {
+    const int b = b0 + lane;
+    unsigned columns = 0, pieces = 1;
+    tiles = 0;
+    if (b < c.B) columns = size_of(b, &tiles);
+    if (tiles > each) pieces = (tiles + each - 1) / each;
+    const unsigned n = columns * c.Hkv * pieces;
+    unsigned run = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const unsigned v = __shfl_up(run, o, 64);
+      if (lane >= o) run += v;
     }
-    at.a += n;
-    at.b += pieces > 1 ? n : 0;
+    const unsigned long long past = __ballot(id < run);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      const unsigned i = id - (__builtin_amdgcn_readlane(run, at) - __builtin_amdgcn_readlane(n, at));
+      const unsigned ps = __builtin_amdgcn_readlane(pieces, at), cs = __builtin_amdgcn_readlane(columns, at), pair = i / ps;
+      w->b = b0 + at;
+      w->piece = (int)(i - pair * ps);
+      w->pieces = (int)ps;
+      w->h = (int)(pair / cs);
+      w->tile = (int)(pair % cs);
+      w->slot = (int)number;
+      return true;
+    }
+    id -= __builtin_amdgcn_readlane(run, 63);
   }
-  __syncthreads();
-  if (by_pair) {
-    w->pieces = found.pieces;
-    w->slot = found.slot;
-  } else {
-    *w = found;
-  }
-  return true;
+  return false;
+}
+// What pieces leave: for every (sequence, head, column tile) its first piece and their number, then for every piece sums of `width` columns, largest scores
+// and sums of weights.
+__device__ __forceinline__ int64_t piece_at(int pairs, int width, int dh, int64_t slot) {
+  return ((pairs * 2 + 15) & ~15) + slot * width * (dh + 2);
+}
+__device__ __forceinline__ void note_pieces(const CacheView& c, const AttnArgs& a, const Work& w) {
+  if (w.piece == 0 && threadIdx.x == 0)
+    reinterpret_cast<int2*>(a.part)[((int64_t)w.b * c.Hkv + w.h) * a.tiles + w.tile] = make_int2(w.slot, w.pieces);
 }
 // Tiles of a piece: [first, last).
 __device__ __forceinline__ void tiles_of(int tiles, int piece, int pieces, int* first, int* last) {
@@ -198,42 +165,88 @@ __device__ __forceinline__ float over(float m, float l) {
 }
 __device__ __forceinline__ float log_sum(float m, float l) { return m == -INFINITY && l <= 0.f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2; }
 
-// ND: head size in units of 64 columns, rounded up.  NC: column tiles of 16.
-template <typename T, int ND, int NC>
-__global__ void __launch_bounds__(64 * kWaves) k_cache_attn(CacheView c, AttnArgs a) {
+// ND: head size in units of 64 columns, rounded up.  NC: column tiles of 16.  W: waves, each with every W-th tile of 64 tokens.  The keys of the
+// next tile are on their way while one is worked on, and the page numbers of the one after that; its values while its scores are computed.
+template <typename T, int ND, int NC, int W>
+__global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cache_attn(CacheView c, AttnArgs a) {
   constexpr int QP = std::is_same<T, float>::value ? 3 : 1, WP = std::is_same<T, float>::value ? 3 : 2, NJ = 4 * ND;
-  constexpr int kPad = 64 * ND + 4;
+  constexpr int kPad = 64 * ND + 4, width = 16 * NC;
   // the queries, and when the axis is done what waves hand to each other
-  constexpr int kQueries = NC * ND * 2 * QP * 64 * 16, kJoin = kWaves / 2 * 16 * (kPad + 2) * 4;
+  constexpr int kQueries = NC * ND * 2 * QP * 64 * 16, kJoin = W / 2 * 16 * (kPad + 2) * 4;
   __shared__ __align__(16) char lds[kQueries > kJoin ? kQueries : kJoin];
   auto sq = reinterpret_cast<bf16x8(*)[64]>(lds);
   auto so = reinterpret_cast<float(*)[16][kPad]>(lds);
-  auto sml = reinterpret_cast<float(*)[2][16]>(lds + kWaves / 2 * 16 * kPad * 4);
+  auto sml = reinterpret_cast<float(*)[2][16]>(lds + W / 2 * 16 * kPad * 4);
   Work w;
-  if (!find_work(c, a, 16 * NC, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, false, &w)) return;
+  const unsigned id = blockIdx.y * gridDim.x + blockIdx.x;
+  if (a.target) {
+    if (!find_work(c, a, width, id, &w)) return;
+    note_pieces(c, a, w);
+  } else {
+    w.tile = (int)(id % a.tiles);
+    w.h = (int)(id / a.tiles % c.Hkv);
+    w.b = (int)(id / a.tiles / c.Hkv);
+    w.piece = w.slot = 0;
+    w.pieces = 1;
+    if (w.b >= c.B) return;
+  }
   const Sequence s = sequence_of(c, w.b);
-  const int col0 = w.tile * 16 * NC;
-  if ((int64_t)col0 >= (int64_t)s.n * a.G) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+  const int col0 = w.tile * width, columns = s.n * a.G;
+  if (col0 >= columns) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
   const int dh = c.dh, page = 1 << c.shift;
 
+  // visible tokens of the lane's columns (0: none), of the first and of the last column there is
+  auto limit = [&](int t) {
+    const int v = a.causal ? s.len - s.n + t + 1 : s.len;
+    return v < 0 ? 0 : v;
+  };
+  const int lo = limit(col0 / a.G), hi = limit((col0 + width < columns ? col0 + width - 1 : columns - 1) / a.G);
+  int tile, last;
+  tiles_of((((a.target ? s.len : hi) + 63) >> 6), w.piece, w.pieces, &tile, &last);
+  if (last > (hi + 63) >> 6) last = (hi + 63) >> 6;
+  tile += wave;
+
+  struct Pages { int k, v; };            // of the tokens whose keys, and whose scores and values, the lane has
+  struct Keys { uint4 k[4][ND]; };
+  auto pages_of = [&](int t) {
+    const int kt = t * 64 + 16 * (i >> 2), vt = t * 64 + 16 * g;
+    return Pages{kt < hi ? page_of(c, w.b, kt >> c.shift) : -1, vt < hi ? page_of(c, w.b, vt >> c.shift) : -1};
+  };
+  auto load = [&](int t, const Pages& p, Keys& x) {
+    const int kt = t * 64 + 16 * (i >> 2);
+    const uint8_t* kp = c.k + ((((int64_t)(p.k < 0 ? 0 : p.k) * c.Hkv + w.h) << c.shift) + (kt & (page - 1)) + (i & 3)) * dh;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int cc = 0; cc < ND; ++cc) {
+        const int d = cc * 64 + g * 16;
+        x.k[u][cc] = p.k >= 0 && d < dh ? *reinterpret_cast<const uint4*>(kp + u * 4 * dh + d) : make_uint4(0, 0, 0, 0);
+      }
+  };
+  Keys one, two;
+  Pages now{-1, -1}, ahead{-1, -1};
+  if (tile < last) {
+    now = pages_of(tile);
+    load(tile, now, one);
+    if (tile + W < last) ahead = pages_of(tile + W);
+  }
+
   // queries, as they enter the products
-  for (int f = wave; f < NC * ND * 2; f += kWaves) {
+  int lim[NC];
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    const Column col = column_of(s, a, w.h, col0 + n * 16 + i);
+    lim[n] = col.there ? limit(col.t) : 0;
+  }
+  for (int f = wave; f < NC * ND * 2; f += W) {
     const int half = f & 1, cc = f / 2 % ND, n = f / (2 * ND), d = cc * 64 + g * 16 + half * 8;
     const Column col = column_of(s, a, w.h, col0 + n * 16 + i);
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (col.there && d < dh) {
       const T* p = (const T*)a.q + col.row * a.ldq + col.head * dh + d;
       if (a.vec) {
-        if constexpr (QP == 1) {
-          const bf16x8 t = *reinterpret_cast<const bf16x8*>(p);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
-        } else {
-          const f32x4 t = *reinterpret_cast<const f32x4*>(p), u = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { v[e] = t[e]; v[4 + e] = u[e]; }
-        }
+        load8(p, v);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = to_f(p[e]);
@@ -246,26 +259,6 @@ __global__ void __launch_bounds__(64 * kWaves) k_cache_attn(CacheView c, AttnArg
   }
   __syncthreads();
 
-  // visible tokens of the lane's columns (0: none), of the first and of the last column there is
-  int lim[NC], lo, hi;
-  {
-    const int most = s.n * a.G - 1, end = col0 + 16 * NC - 1 < most ? col0 + 16 * NC - 1 : most;
-    auto limit = [&](int t) {
-      const int v = a.causal ? s.len - s.n + t + 1 : s.len;
-      return v < 0 ? 0 : v;
-    };
-    lo = limit(col0 / a.G);
-    hi = limit(end / a.G);
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      const Column col = column_of(s, a, w.h, col0 + n * 16 + i);
-      lim[n] = col.there ? limit(col.t) : 0;
-    }
-  }
-  int tile, last;
-  tiles_of((((a.target ? s.len : hi) + 63) >> 6), w.piece, w.pieces, &tile, &last);
-  if (last > (hi + 63) >> 6) last = (hi + 63) >> 6;
-
   f32x4 acc[NC][NJ];
   float m[NC], l[NC];
   bool seen[NC];
@@ -277,52 +270,41 @@ __global__ void __launch_bounds__(64 * kWaves) k_cache_attn(CacheView c, AttnArg
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  for (tile += wave; tile < last; tile += kWaves) {
-    const int tok = tile * 64, kt = tok + 16 * (i >> 2), vt = tok + 16 * g;
-    const int pk = kt < hi ? page_of(c, w.b, kt >> c.shift) : -1, pv = vt < hi ? page_of(c, w.b, vt >> c.shift) : -1;
-    uint4 kr[4][ND], vr[NJ];
-    {
-      const uint8_t* p = c.k + ((((int64_t)(pk < 0 ? 0 : pk) * c.Hkv + w.h) << c.shift) + (kt & (page - 1)) + (i & 3)) * dh;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int cc = 0; cc < ND; ++cc) {
-          const int d = cc * 64 + g * 16;
-          kr[t][cc] = pk >= 0 && d < dh ? *reinterpret_cast<const uint4*>(p + t * 4 * dh + d) : make_uint4(0, 0, 0, 0);
-        }
-    }
+  auto attend = [&](int t, const Keys& x, Keys& next) {
+    const int tok = t * 64, vt = tok + 16 * g, pv = now.v;
+    uint4 vr[NJ];
     float ks = 0.f, vs = 0.f;
     {
       const int64_t where = (int64_t)(pv < 0 ? 0 : pv) * c.Hkv + w.h;
-      const uint8_t* p = c.v + ((where * dh + i) << c.shift) + (vt & (page - 1));
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) vr[j] = pv >= 0 && j * 16 < dh ? *reinterpret_cast<const uint4*>(p + (j * 16 << c.shift)) : make_uint4(0, 0, 0, 0);
+      const uint8_t* vp = c.v + ((where * dh + i) << c.shift) + (vt & (page - 1));
       if (pv >= 0) {
         ks = c.ks[where] * a.scale;
         vs = c.vs[where];
       }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) vr[j] = pv >= 0 && j * 16 < dh ? *reinterpret_cast<const uint4*>(vp + (j * 16 << c.shift)) : make_uint4(0, 0, 0, 0);
+    }
+    if (t + W < last) {
+      load(t + W, ahead, next);
+      now = ahead;
+      if (t + 2 * W < last) ahead = pages_of(t + 2 * W);
     }
     const bool masked = tok + 64 > lo || __ballot(pv < 0) != 0;
-
     f32x4 sc[NC][4];
-#pragma unroll
-    for (int n = 0; n < NC; ++n)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) sc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int cc = 0; cc < ND; ++cc)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         bf16x8 kf[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) kf[t] = half ? codes8(kr[t][cc].z, kr[t][cc].w) : codes8(kr[t][cc].x, kr[t][cc].y);
+        for (int u = 0; u < 4; ++u) kf[u] = half ? codes8(x.k[u][cc].z, x.k[u][cc].w) : codes8(x.k[u][cc].x, x.k[u][cc].y);
 #pragma unroll
         for (int n = 0; n < NC; ++n)
 #pragma unroll
           for (int q = QP - 1; q >= 0; --q) {
             const bf16x8 qf = sq[((n * ND + cc) * 2 + half) * QP + q][lane];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) sc[n][t] = mma(kf[t], qf, sc[n][t]);
+            for (int u = 0; u < 4; ++u) sc[n][u] = mma(kf[u], qf, cc == 0 && half == 0 && q == QP - 1 ? f32x4{} : sc[n][u]);
           }
       }
 
@@ -331,17 +313,17 @@ __global__ void __launch_bounds__(64 * kWaves) k_cache_attn(CacheView c, AttnArg
     for (int n = 0; n < NC; ++n) {
       float top = -INFINITY;
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float x = sc[n][t][r] * ks;
+          float y = sc[n][u][r] * ks;
           if (masked) {
-            const bool ok = vt + t * 4 + r < lim[n] && pv >= 0;
-            x = ok ? x : -INFINITY;
+            const bool ok = vt + u * 4 + r < lim[n] && pv >= 0;
+            y = ok ? y : -INFINITY;
             seen[n] |= ok;
           }
-          sc[n][t][r] = x;
-          top = fmaxf(top, x);
+          sc[n][u][r] = y;
+          top = fmaxf(top, y);
         }
       if (!masked) seen[n] = true;
       top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -422,6 +404,10 @@ __global__ void __launch_bounds__(64 * kWaves) k_cache_attn(CacheView c, AttnArg
           acc[n][j] = mma(v1, wf[n][1][q], acc[n][j]);
         }
     }
+  };
+  for (; tile < last; tile += 2 * W) {
+    attend(tile, one, two);
+    if (tile + W < last) attend(tile + W, two, one);
   }
 
   // the four lanes of a column, then the waves, two by two
@@ -433,7 +419,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_cache_attn(CacheView c, AttnArg
     any |= __shfl_xor(any, 16, 64);
     any |= __shfl_xor(any, 32, 64);
     if (any && m[n] == -INFINITY && l[n] == 0.f) l[n] = -1.f;
-    for (int step = kWaves / 2; step > 0; step >>= 1) {
+    for (int step = W / 2; step > 0; step >>= 1) {
       __syncthreads();
       if (wave >= step && wave < 2 * step) {
         if (g == 0) { sml[wave - step][0][i] = m[n]; sml[wave - step][1][i] = l[n]; }
@@ -453,16 +439,14 @@ __global__ void __launch_bounds__(64 * kWaves) k_cache_attn(CacheView c, AttnArg
     }
     if (wave != 0) continue;
     const Column col = column_of(s, a, w.h, col0 + n * 16 + i);
+    if (!col.there) continue;
     if (w.pieces > 1) {
-      float* out = a.part + ((int64_t)w.slot * 16 * NC + n * 16 + i) * (dh + 2);
-      if (g == 0) { out[dh] = m[n]; out[dh + 1] = l[n]; }
+      float* out = a.part + piece_at(c.B * c.Hkv * a.tiles, width, dh, w.slot);
+      if (g == 0) *reinterpret_cast<float2*>(out + width * dh + (n * 16 + i) * 2) = make_float2(m[n], l[n]);
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
-        if (j * 16 < dh) {
-          *reinterpret_cast<float2*>(out + j * 16 + g * 4) = make_float2(acc[n][j][0], acc[n][j][1]);
-          *reinterpret_cast<float2*>(out + j * 16 + g * 4 + 2) = make_float2(acc[n][j][2], acc[n][j][3]);
-        }
-    } else if (col.there) {
+        if (j * 16 < dh) *reinterpret_cast<f32x4*>(out + (n * 16 + i) * dh + j * 16 + g * 4) = acc[n][j];
+    } else {
       const float f = over(m[n], l[n]);
       T* out = (T*)a.o + col.row * a.ldo + col.head * dh;
       if (a.lse && g == 0) a.lse[col.row * a.H + col.head] = log_sum(m[n], l[n]);
@@ -514,10 +498,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // NB: head size in units of 32 columns, rounded up; CG: column groups of 32 of a wave.
-template <typename T, int NB, int CG>
-__global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
+template <typename T, int NB>
+__global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
   constexpr bool F = std::is_same<T, float>::value;
-  constexpr int QP = F ? 3 : 1, WP = F ? 2 : 1, DH = 32 * NB, KLD = DH + 8, VLD = 72, kLoads = (64 * (DH / 16) + 255) / 256;
+  constexpr int CG = 1, QP = F ? 3 : 1, WP = F ? 2 : 1, DH = 32 * NB, KLD = DH + 8, VLD = 72, kLoads = (64 * (DH / 16) + 255) / 256;
   constexpr float kTop = 7.f, kLag = 8.f;
   __shared__ __align__(16) bf16_t sk[2][64][KLD];
   __shared__ __align__(16) _Float16 sv[2][DH][VLD];
@@ -527,7 +511,8 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
   const int dh = c.dh, page = 1 << c.shift, width = 128 * CG;
   Work w;
   if (a.target) {
-    if (!find_work(c, a, width, id, false, &w)) return;
+    if (!find_work(c, a, width, (unsigned)id, &w)) return;
+    note_pieces(c, a, w);
   } else {
     // the longest first; a head's column tiles in turn on the eight parts of the chip, so that sequences of different lengths load them alike
     const int pairs = c.B * c.Hkv, turn = (int)(id / pairs);
@@ -809,19 +794,19 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
     const Column col = column_of(s, a, w.h, at);
     // from the weights' reference to the scores'
     const float back = top[n] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[n] - m[n] - kTop);
+    if (!col.there) continue;
     if (w.pieces > 1) {
-      float* out = a.part + ((int64_t)w.slot * width + at - col0) * (dh + 2);
-      if (half == 0) { out[dh] = m[n]; out[dh + 1] = l[n]; }
+      float* out = a.part + piece_at(c.B * c.Hkv * a.tiles, width, dh, w.slot);
+      if (half == 0) *reinterpret_cast<float2*>(out + width * dh + (at - col0) * 2) = make_float2(m[n], l[n]);
 #pragma unroll
       for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int v = 0; v < 16; v += 4) {
           const int d = j * 32 + 2 * v + 4 * half;
-          if (d >= dh) continue;
-          *reinterpret_cast<float2*>(out + d) = make_float2(acc[n][j][v] * back, acc[n][j][v + 1] * back);
-          *reinterpret_cast<float2*>(out + d + 2) = make_float2(acc[n][j][v + 2] * back, acc[n][j][v + 3] * back);
+          if (d < dh)
+            *reinterpret_cast<f32x4*>(out + (at - col0) * dh + d) = f32x4{acc[n][j][v] * back, acc[n][j][v + 1] * back, acc[n][j][v + 2] * back, acc[n][j][v + 3] * back};
         }
-    } else if (col.there) {
+    } else {
       const float f = over(m[n], l[n]) * back;
       T* out = (T*)a.o + col.row * a.ldo + col.head * dh;
       if (a.lse && half == 0) a.lse[col.row * a.H + col.head] = log_sum(m[n], l[n]);
@@ -838,41 +823,68 @@ __global__ void __launch_bounds__(256, NB * CG <= 4 && sizeof(T) == 2 ? 2 : 1) k
 }
 
 // ------------------------------------------------------------------------------------------------ divided axes
-// The pieces of a divided axis, in their order.
-template <typename T>
+// The pieces of a divided axis, in their order.  A column belongs to a wave, or to the four of a block; a quad of its columns of the head to one lane
+// for every so many pieces.
+template <typename T, int WAVES>
 __global__ void __launch_bounds__(256) k_cache_join(CacheView c, AttnArgs a, int width) {
-  Work w;
-  if (!find_work(c, a, width, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, true, &w) || w.pieces < 2) return;
-  const Sequence s = sequence_of(c, w.b);
-  const int dh = c.dh, quads = dh / 4;
-  for (int it = threadIdx.x; it < width * quads; it += 256) {
-    const int n = it / quads, d = (it - n * quads) * 4;
-    const Column col = column_of(s, a, w.h, w.tile * width + n);
-    if (!col.there) continue;
-    const float* p = a.part + ((int64_t)w.slot * width + n) * (dh + 2);
-    const int64_t step = (int64_t)width * (dh + 2);
-    float top = -INFINITY;
-    for (int i = 0; i < w.pieces; ++i) top = fmaxf(top, p[i * step + dh]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float l = 0.f;
-    bool none = false;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < w.pieces; ++i) {
-      const float* q = p + i * step;
-      const float f = __builtin_amdgcn_exp2f(q[dh] - base), li = q[dh + 1];
-      none |= li < 0.f;
-      l += li < 0.f ? 0.f : top == -INFINITY ? li : li * f;
-      const float2 x = *reinterpret_cast<const float2*>(q + d), y = *reinterpret_cast<const float2*>(q + d + 2);
-      o[0] += x.x * f; o[1] += x.y * f; o[2] += y.x * f; o[3] += y.y * f;
-    }
-    if (none && top == -INFINITY && l == 0.f) l = -1.f;
-    if (a.lse && d == 0) a.lse[col.row * a.H + col.head] = log_sum(top, l);
-    put4((T*)a.o + col.row * a.ldo + col.head * dh + d, o * over(top, l), a.vec);
+  __shared__ f32x4 sh[4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), dh = c.dh;
+  const unsigned id = blockIdx.y * gridDim.x + blockIdx.x, groups = width * WAVES / 4, pair = id / groups, pairs = c.B * c.Hkv * a.tiles;
+  if (pair >= pairs) return;
+  const int n = (int)(id - pair * groups) * (4 / WAVES) + (WAVES == 4 ? 0 : wave);
+  const int tile = (int)(pair % a.tiles), h = (int)(pair / a.tiles % c.Hkv), b = (int)(pair / a.tiles / c.Hkv);
+  const Sequence s = sequence_of(c, b);
+  const Column col = column_of(s, a, h, tile * width + n);
+  if (!col.there) return;                                          // with four waves a column: all of them
+  const int2 which = reinterpret_cast<const int2*>(a.part)[pair];
+  const int pieces = which.y;
+  if (pieces < 2) return;
+  const int64_t step = (int64_t)width * (dh + 2);
+  const float* p = a.part + piece_at(pairs, width, dh, which.x);
+  const float* ml = p + width * dh + n * 2;
+  float top = -INFINITY;
+  for (int i = lane; i < pieces; i += 64) top = fmaxf(top, ml[i * step]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  const float base = top == -INFINITY ? 0.f : top;
+  float l = 0.f;
+  int none = 0;
+  for (int i = lane; i < pieces; i += 64) {
+    const float2 x = *reinterpret_cast<const float2*>(ml + i * step);
+    none |= x.y < 0.f;
+    l += x.y < 0.f ? 0.f : top == -INFINITY ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - base);
   }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    l += __shfl_xor(l, o, 64);
+    none |= __shfl_xor(none, o, 64);
+  }
+  if (none && top == -INFINITY && l == 0.f) l = -1.f;
+
+  const int quads = dh <= 16 ? 4 : dh <= 32 ? 8 : dh <= 64 ? 16 : dh <= 128 ? 32 : 64;
+  const int d = (lane & (quads - 1)) * 4, first = lane / quads + (WAVES == 4 ? wave * (64 / quads) : 0), stride = 64 / quads * WAVES;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  if (d < dh) {
+#pragma unroll 4
+    for (int i = first; i < pieces; i += stride)
+      o += *reinterpret_cast<const f32x4*>(p + i * step + n * dh + d) * __builtin_amdgcn_exp2f(ml[i * step] - base);
+  }
+  for (int q = quads; q < 64; q <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], q, 64);
+  if constexpr (WAVES == 4) {
+    sh[wave][lane] = o;
+    __syncthreads();
+    if (wave) return;
+    o = sh[0][lane] + sh[1][lane] + sh[2][lane] + sh[3][lane];
+  }
+  if (lane >= quads || d >= dh) return;
+  if (a.lse && d == 0) a.lse[col.row * a.H + col.head] = log_sum(top, l);
+  put4((T*)a.o + col.row * a.ldo + col.head * dh + d, o * over(top, l), a.vec);
 }
 
 // The kernel, the columns of a block, and the pieces that axes are cut into.
-struct Shape { bool prompt; int nc, width, tiles, target; };
+struct Shape { bool prompt; int nc, waves, width, tiles, target; };
 Shape shape_of(int B, int T, int H, int Hkv, int dh, int64_t tokens) {
   Shape s;
   const int64_t columns = (int64_t)T * (H / Hkv);
@@ -880,12 +892,17 @@ Shape shape_of(int B, int T, int H, int Hkv, int dh, int64_t tokens) {
   s.prompt = columns > 64;
   s.nc = s.prompt ? 1 : columns <= 16 ? 1 : columns <= 32 ? 2 : 4;
   if (s.nc > most) s.nc = most;
-  s.width = s.prompt ? 128 * s.nc : 16 * s.nc;
+  s.width = s.prompt ? 128 : 16 * s.nc;
   s.tiles = (int)((columns + s.width - 1) / s.width);
   const int64_t pairs = (int64_t)B * Hkv * s.tiles, longest = (tokens + 63) / 64;
+  s.waves = kWaves;
   s.target = s.prompt ? 512 : 1024;
-  // nothing to cut: short axes, or more of them than blocks are wanted
-  if (longest <= 2 * kWaves || pairs >= (s.prompt ? s.target : 4 * s.target) || B > 1 << 16) s.target = 0;
+  if (!s.prompt && s.nc == 1 && dh <= 128 && longest <= 32 && pairs <= 256) {
+    s.waves = 8;
+    s.target = 0;
+  }
+  // nothing to cut: short axes, or more of them than blocks are wanted; sums are of 32 bits
+  if (longest <= 2 * kWaves || pairs >= (s.prompt ? s.target : 4 * s.target) || pairs * longest >= (int64_t)1 << 31) s.target = 0;
   else if (pairs * ((longest + kWaves - 1) / kWaves) < s.target) s.target = (int)(pairs * ((longest + kWaves - 1) / kWaves));
   return s;
 }
@@ -903,7 +920,8 @@ bool cache_attn_ok(int B, int T, int H, int Hkv, int dh, int page, int max_pages
 size_t cache_attn_scratch(int B, int T, int H, int Hkv, int dh, int page, int max_pages) {
   if (!cache_attn_ok(B, T, H, Hkv, dh, page, max_pages)) return 0;
   const Shape s = shape_of(B, T, H, Hkv, dh, (int64_t)max_pages * page);
-  return (size_t)2 * s.target * s.width * (dh + 2);
+  const int64_t pairs = (int64_t)B * Hkv * s.tiles;
+  return s.target ? (size_t)((pairs * 2 + 15) & ~(int64_t)15) + (size_t)(pairs + s.target) * s.width * (dh + 2) : 0;
 }
 
 hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse, int H, int causal) {
@@ -913,13 +931,10 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
   if (ldq < width || ldo < width || ldq > widest || ldo > widest) return hipErrorInvalidValue;
   if (view.B == 0 || view.rows == 0) return hipSuccess;
   if (!q || !o || !cache_operands_ok(view)) return hipErrorInvalidValue;
-  Shape s = shape_of(view.B, view.T, H, view.Hkv, dh, (int64_t)view.max_pages * page);
+  const Shape s = shape_of(view.B, view.T, H, view.Hkv, dh, (int64_t)view.max_pages * page);
   const size_t need = cache_attn_scratch(view.B, view.T, H, view.Hkv, dh, page, view.max_pages);
-  if (need && (!c.partial || c.partial_elems < need || ((uintptr_t)c.partial & 7))) return hipErrorInvalidValue;
+  if (need && (!c.partial || c.partial_elems < need || ((uintptr_t)c.partial & 15))) return hipErrorInvalidValue;
   const int G = H / view.Hkv;
-  // 64 columns a wave
-  const bool wide = false && s.prompt && !s.target && c.dt == BF16 && dh <= 64;
-  if (wide) s.tiles = (int)(((int64_t)view.T * G + 255) / 256);
   AttnArgs a{q, o, lse, c.partial, ldq, ldo, H, G, causal != 0, s.tiles, s.target,
              ldq % 8 == 0 && ldo % 8 == 0 && (((uintptr_t)q | (uintptr_t)o) & 15) == 0, kLog2e / sqrtf((float)dh)};
   const int64_t pairs = (int64_t)view.B * view.Hkv * s.tiles;
@@ -928,24 +943,31 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
     return dim3((unsigned)(blocks < most ? blocks : most), (unsigned)((blocks + most - 1) / most));
   };
   if (pairs > (int64_t)1 << 32 || (int64_t)view.B * view.Hkv > 1 << 30) return hipErrorInvalidValue;
+  // with few columns a block joins one of them (there are many pieces), with many four
+  auto join = [&](auto t) {
+    typedef decltype(t) T;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !s.target) return e;
+    if (s.prompt) k_cache_join<T, 1><<<grid(pairs * s.width / 4), 256, 0, c.stream>>>(view, a, s.width);
+    else k_cache_join<T, 4><<<grid(pairs * s.width), 256, 0, c.stream>>>(view, a, s.width);
+    return hipGetLastError();
+  };
   auto go = [&](auto t, auto nd, auto nc) {
     typedef decltype(t) T;
-    k_cache_attn<T, decltype(nd)::value, decltype(nc)::value><<<grid(pairs + s.target), 64 * kWaves, 0, c.stream>>>(view, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !s.target) return e;
-    k_cache_join<T><<<grid(pairs), 256, 0, c.stream>>>(view, a, s.width);
-    return hipGetLastError();
+    constexpr int ND = decltype(nd)::value, NC = decltype(nc)::value;
+    if constexpr (NC == 1 && ND <= 2) {
+      if (s.waves == 8) {
+        k_cache_attn<T, ND, NC, 8><<<grid(pairs), 512, 0, c.stream>>>(view, a);
+        return join(t);
+      }
+    }
+    k_cache_attn<T, ND, NC, kWaves><<<grid(pairs + s.target), 64 * kWaves, 0, c.stream>>>(view, a);
+    return join(t);
   };
   auto many = [&](auto t, auto nb) {
     typedef decltype(t) T;
-    constexpr int NB = decltype(nb)::value, most = NB <= 2 && std::is_same<T, bf16_t>::value ? 2 : 1;
-    const int64_t blocks = pairs + s.target;
-    if (wide) k_cache_prompt<T, NB, most><<<grid(blocks), 256, 0, c.stream>>>(view, a);
-    else k_cache_prompt<T, NB, 1><<<grid(blocks), 256, 0, c.stream>>>(view, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !s.target) return e;
-    k_cache_join<T><<<grid(pairs), 256, 0, c.stream>>>(view, a, s.width);
-    return hipGetLastError();
+    k_cache_prompt<T, decltype(nb)::value><<<grid(pairs + s.target), 256, 0, c.stream>>>(view, a);
+    return join(t);
   };
   auto by_columns = [&](auto t, auto nd) {
     constexpr int ND = decltype(nd)::value;
