@@ -29,6 +29,7 @@ struct AttnArgs {
   float *lse, *part;        // part: what the pieces of a divided axis leave
   int64_t ldq, ldo;
   int H, G, causal, tiles;  // tiles: column tiles of a sequence, at most
+  unsigned by_g;            // 2^32 / G, rounded up: quotients of numbers below 2^12 by products; not for 1
   int target;               // pieces that the axes are divided into, about (0: none is divided)
   bool vec;
   float scale;
@@ -64,8 +65,26 @@ __device__ __forceinline__ unsigned nan_bytes(unsigned w) {
   return (hit >> 7) * 0xffu;
 }
 
+// The largest of three; NaN count only where there is nothing else.  (As an instruction of its own: in C each operand would be made quiet first.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 // What a block works on.
 struct Work { int b, h, tile, piece, pieces, slot; };
+
+// Sums over the lanes up to a lane's own; the last one's is the sum of all.  (Sixteen by sixteen lanes, then across: 6 additions without LDS.)
+__device__ __forceinline__ unsigned running_sum(unsigned v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // lanes 1, 2, 4 and 8 before, in a row of sixteen
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // a row's last lane to the next row, in rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // lane 31 to rows 2 and 3
+  return v;
+}
 
 // The axes are cut so that all pieces have the same number of tiles, whatever the sequences' lengths: as many as leave about `target` pieces in
 // all.  Pieces are numbered through sequences, heads, column tiles and the axis; this finds piece `id`, alike in every wave and without a barrier.  The host has
@@ -78,43 +97,37 @@ __device__ __forceinline__ bool find_work(const CacheView& c, const AttnArgs& a,
     *tiles = (unsigned)(s.len + 63) >> 6;
     return ((unsigned)s.n * a.G + width - 1) / width;
   };
-  unsigned all = 0, tiles = 0;
+  unsigned all = 0, tiles = 0, columns = 0;
   for (int b = lane; b < c.B; b += 64) {
-    const unsigned columns = size_of(b, &tiles);
+    columns = size_of(b, &tiles);
     all += columns * tiles;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o, 64);
-  all = __builtin_amdgcn_readfirstlane(all) * c.Hkv;
+  all = (unsigned)__builtin_amdgcn_readlane((int)running_sum(all), 63) * c.Hkv;
   unsigned each = (all + a.target - 1) / a.target;
   if (each < kWaves) each = kWaves;
   for (int b0 = 0; b0 < c.B; b0 += 64) {
     const int b = b0 + lane;
-    unsigned columns = 0, pieces = 1;
-    tiles = 0;
-    if (b < c.B) columns = size_of(b, &tiles);
-    if (tiles > each) pieces = (tiles + each - 1) / each;
-    const unsigned n = columns * c.Hkv * pieces;
-    unsigned run = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const unsigned v = __shfl_up(run, o, 64);
-      if (lane >= o) run += v;
+    if (c.B > 64) {
+      columns = tiles = 0;
+      if (b < c.B) columns = size_of(b, &tiles);
     }
+    const unsigned pieces = tiles > each ? (tiles + each - 1) / each : 1;
+    const unsigned n = columns * c.Hkv * pieces, run = running_sum(n);
     const unsigned long long past = __ballot(id < run);
     if (past) {
       const int at = __builtin_ctzll(past);
-      const unsigned i = id - (__builtin_amdgcn_readlane(run, at) - __builtin_amdgcn_readlane(n, at));
-      const unsigned ps = __builtin_amdgcn_readlane(pieces, at), cs = __builtin_amdgcn_readlane(columns, at), pair = i / ps;
+      const unsigned i = id - (unsigned)(__builtin_amdgcn_readlane((int)run, at) - __builtin_amdgcn_readlane((int)n, at));
+      const unsigned ps = __builtin_amdgcn_readlane((int)pieces, at), cs = __builtin_amdgcn_readlane((int)columns, at);
+      const unsigned pair = ps == 1 ? i : i / ps, h = cs == 1 ? pair : pair / cs;
       w->b = b0 + at;
       w->piece = (int)(i - pair * ps);
       w->pieces = (int)ps;
-      w->h = (int)(pair / cs);
-      w->tile = (int)(pair % cs);
+      w->h = (int)h;
+      w->tile = (int)(pair - h * cs);
       w->slot = (int)number;
       return true;
     }
-    id -= __builtin_amdgcn_readlane(run, 63);
+    id -= (unsigned)__builtin_amdgcn_readlane((int)run, 63);
   }
   return false;
 }
@@ -165,27 +178,42 @@ __device__ __forceinline__ float over(float m, float l) {
 }
 __device__ __forceinline__ float log_sum(float m, float l) { return m == -INFINITY && l <= 0.f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2; }
 
-// ND: head size in units of 64 columns, rounded up.  NC: column tiles of 16.  W: waves, each with every W-th tile of 64 tokens.  The keys of the
-// next tile are on their way while one is worked on, and the page numbers of the one after that; its values while its scores are computed.
-template <typename T, int ND, int NC, int W>
+// The larger of the numbers of the four lanes of a column.
+__device__ __forceinline__ float max_of_column(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const unsigned x = r[0], y = r[1];         // copied: a bit cast straight from a vector's element takes the first one
+  const float m = fmaxf(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y));
+  const unsigned n = __builtin_bit_cast(unsigned, m);
+  const auto q = __builtin_amdgcn_permlane16_swap(n, n, false, false);
+  const unsigned e = q[0], f = q[1];
+  return fmaxf(__builtin_bit_cast(float, e), __builtin_bit_cast(float, f));
+}
+
+// ND: head size in units of 64 columns, rounded up.  NC: column tiles of 16.  W: waves, each with every W-th tile of 64 tokens.  ONE: a tile is in one
+// page (pages of 64 tokens or more), whose address is a scalar; otherwise each lane finds its runs' pages.  The keys of the next tile are on their way while one is
+// worked on, and the page number of the one after that; its values while its scores are computed.  Loads are never skipped: where there is no page, page 0
+// is read and its scores and values are taken out, and columns behind the head's repeat its last sixteen, against zeros of the query.
+template <typename T, int ND, int NC, int W, bool ONE>
 __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cache_attn(CacheView c, AttnArgs a) {
   constexpr int QP = std::is_same<T, float>::value ? 3 : 1, WP = std::is_same<T, float>::value ? 3 : 2, NJ = 4 * ND;
-  constexpr int kPad = 64 * ND + 4, width = 16 * NC;
+  constexpr int kPad = 64 * ND + 4, width = 16 * NC, kFrags = (NC * ND * 2 + W - 1) / W;
   // the queries, and when the axis is done what waves hand to each other
-  constexpr int kQueries = NC * ND * 2 * QP * 64 * 16, kJoin = W / 2 * 16 * (kPad + 2) * 4;
+  constexpr int kQueries = NC * ND * 2 * QP * 64 * 16, kJoin = W * width * (kPad + 2) * 4;
   __shared__ __align__(16) char lds[kQueries > kJoin ? kQueries : kJoin];
   auto sq = reinterpret_cast<bf16x8(*)[64]>(lds);
-  auto so = reinterpret_cast<float(*)[16][kPad]>(lds);
-  auto sml = reinterpret_cast<float(*)[2][16]>(lds + W / 2 * 16 * kPad * 4);
+  auto so = reinterpret_cast<float(*)[width][kPad]>(lds);
+  auto sml = reinterpret_cast<float2(*)[width]>(lds + W * width * kPad * 4);
   Work w;
   const unsigned id = blockIdx.y * gridDim.x + blockIdx.x;
   if (a.target) {
     if (!find_work(c, a, width, id, &w)) return;
     note_pieces(c, a, w);
   } else {
-    w.tile = (int)(id % a.tiles);
-    w.h = (int)(id / a.tiles % c.Hkv);
-    w.b = (int)(id / a.tiles / c.Hkv);
+    const unsigned pair = a.tiles == 1 ? id : id / a.tiles;
+    w.tile = (int)(id - pair * a.tiles);
+    w.b = (int)(pair / c.Hkv);
+    w.h = (int)(pair - w.b * c.Hkv);
     w.piece = w.slot = 0;
     w.pieces = 1;
     if (w.b >= c.B) return;
@@ -195,34 +223,76 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cac
   if (col0 >= columns) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
   const int dh = c.dh, page = 1 << c.shift;
-
-  // visible tokens of the lane's columns (0: none), of the first and of the last column there is
+  const int64_t page_bytes = (int64_t)c.Hkv * dh << c.shift;
+  // a column's token among the new ones: there are few columns, so that the quotient by G is a product
+  auto new_of = [&](int col) { return a.G == 1 ? col : (int)__umulhi((unsigned)col, a.by_g); };
   auto limit = [&](int t) {
     const int v = a.causal ? s.len - s.n + t + 1 : s.len;
     return v < 0 ? 0 : v;
   };
-  const int lo = limit(col0 / a.G), hi = limit((col0 + width < columns ? col0 + width - 1 : columns - 1) / a.G);
+
+  // queries on their way
+  float qv[kFrags][8];
+#pragma unroll
+  for (int u = 0; u < kFrags; ++u) {
+    const int f = wave + u * W, half = f & 1, cc = f / 2 % ND, d = cc * 64 + g * 16 + half * 8, col = col0 + f / (2 * ND) * 16 + i, t = new_of(col);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) qv[u][e] = 0.f;
+    if (f < NC * ND * 2 && t < s.n && d < dh) {
+      const T* p = (const T*)a.q + (s.first + t) * a.ldq + (w.h * a.G + col - t * a.G) * dh + d;
+      if (a.vec) {
+        load8(p, qv[u]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qv[u][e] = to_f(p[e]);
+      }
+    }
+  }
+
+  // visible tokens of the first and of the last column there is, and of the lane's columns (0: none)
+  const int lo = limit(new_of(col0)), hi = limit(new_of(col0 + width < columns ? col0 + width - 1 : columns - 1));
+  int lim[NC];
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    const int t = new_of(col0 + n * 16 + i);
+    lim[n] = t < s.n ? limit(t) : 0;
+  }
   int tile, last;
-  tiles_of((((a.target ? s.len : hi) + 63) >> 6), w.piece, w.pieces, &tile, &last);
-  if (last > (hi + 63) >> 6) last = (hi + 63) >> 6;
+  if (w.pieces == 1) {
+    tile = 0;
+    last = (hi + 63) >> 6;
+  } else {
+    tiles_of((s.len + 63) >> 6, w.piece, w.pieces, &tile, &last);
+    if (last > (hi + 63) >> 6) last = (hi + 63) >> 6;
+  }
   tile += wave;
 
   struct Pages { int k, v; };            // of the tokens whose keys, and whose scores and values, the lane has
   struct Keys { uint4 k[4][ND]; };
   auto pages_of = [&](int t) {
-    const int kt = t * 64 + 16 * (i >> 2), vt = t * 64 + 16 * g;
-    return Pages{kt < hi ? page_of(c, w.b, kt >> c.shift) : -1, vt < hi ? page_of(c, w.b, vt >> c.shift) : -1};
+    if constexpr (ONE) {
+      const int p = __builtin_amdgcn_readfirstlane(page_of(c, w.b, t * 64 >> c.shift));
+      return Pages{p, p};
+    } else {
+      const int kt = t * 64 + 16 * (i >> 2), vt = t * 64 + 16 * g;
+      return Pages{kt < hi ? page_of(c, w.b, kt >> c.shift) : -1, vt < hi ? page_of(c, w.b, vt >> c.shift) : -1};
+    }
   };
+  const uint8_t *kh = c.k + ((int64_t)w.h * dh << c.shift), *vh = c.v + ((int64_t)w.h * dh << c.shift);
+  unsigned koff[ND];
+#pragma unroll
+  for (int cc = 0; cc < ND; ++cc) {
+    const int d = cc * 64 + g * 16;
+    koff[cc] = (unsigned)((ONE ? 16 * (i >> 2) + (i & 3) : i & 3) * dh + (d < dh ? d : dh - 16));
+  }
+  const unsigned voff = ((unsigned)i << c.shift) + (ONE ? 16 * g : 0);
   auto load = [&](int t, const Pages& p, Keys& x) {
-    const int kt = t * 64 + 16 * (i >> 2);
-    const uint8_t* kp = c.k + ((((int64_t)(p.k < 0 ? 0 : p.k) * c.Hkv + w.h) << c.shift) + (kt & (page - 1)) + (i & 3)) * dh;
+    const int at = (ONE ? t * 64 : t * 64 + 16 * (i >> 2)) & (page - 1);
+    const uint8_t* kp = kh + ((p.k < 0 ? 0 : p.k) * page_bytes + at * dh);
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int cc = 0; cc < ND; ++cc) {
-        const int d = cc * 64 + g * 16;
-        x.k[u][cc] = p.k >= 0 && d < dh ? *reinterpret_cast<const uint4*>(kp + u * 4 * dh + d) : make_uint4(0, 0, 0, 0);
-      }
+      for (int cc = 0; cc < ND; ++cc) x.k[u][cc] = *reinterpret_cast<const uint4*>(kp + u * 4 * dh + koff[cc]);
   };
   Keys one, two;
   Pages now{-1, -1}, ahead{-1, -1};
@@ -232,30 +302,15 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cac
     if (tile + W < last) ahead = pages_of(tile + W);
   }
 
-  // queries, as they enter the products
-  int lim[NC];
 #pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    const Column col = column_of(s, a, w.h, col0 + n * 16 + i);
-    lim[n] = col.there ? limit(col.t) : 0;
-  }
-  for (int f = wave; f < NC * ND * 2; f += W) {
-    const int half = f & 1, cc = f / 2 % ND, n = f / (2 * ND), d = cc * 64 + g * 16 + half * 8;
-    const Column col = column_of(s, a, w.h, col0 + n * 16 + i);
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (col.there && d < dh) {
-      const T* p = (const T*)a.q + col.row * a.ldq + col.head * dh + d;
-      if (a.vec) {
-        load8(p, v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = to_f(p[e]);
-      }
-    }
+  for (int u = 0; u < kFrags; ++u) {
+    const int f = wave + u * W;
     bf16x8 parts[QP];
-    split8<QP>(v, parts);
+    split8<QP>(qv[u], parts);
+    if (f < NC * ND * 2) {
 #pragma unroll
-    for (int q = 0; q < QP; ++q) sq[f * QP + q][lane] = parts[q];
+      for (int q = 0; q < QP; ++q) sq[f * QP + q][lane] = parts[q];
+    }
   }
   __syncthreads();
 
@@ -273,23 +328,22 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cac
   auto attend = [&](int t, const Keys& x, Keys& next) {
     const int tok = t * 64, vt = tok + 16 * g, pv = now.v;
     uint4 vr[NJ];
-    float ks = 0.f, vs = 0.f;
+    float ks, vs;
     {
-      const int64_t where = (int64_t)(pv < 0 ? 0 : pv) * c.Hkv + w.h;
-      const uint8_t* vp = c.v + ((where * dh + i) << c.shift) + (vt & (page - 1));
-      if (pv >= 0) {
-        ks = c.ks[where] * a.scale;
-        vs = c.vs[where];
-      }
+      const int p = pv < 0 ? 0 : pv;
+      const int64_t where = (int64_t)p * c.Hkv + w.h;
+      ks = c.ks[where];
+      vs = c.vs[where];
+      const uint8_t* vp = vh + (p * page_bytes + ((ONE ? tok : vt) & (page - 1)));
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) vr[j] = pv >= 0 && j * 16 < dh ? *reinterpret_cast<const uint4*>(vp + (j * 16 << c.shift)) : make_uint4(0, 0, 0, 0);
+      for (int j = 0; j < NJ; ++j) vr[j] = *reinterpret_cast<const uint4*>(vp + ((j * 16 < dh ? j * 16 : dh - 16) << c.shift) + voff);
     }
     if (t + W < last) {
       load(t + W, ahead, next);
       now = ahead;
       if (t + 2 * W < last) ahead = pages_of(t + 2 * W);
     }
-    const bool masked = tok + 64 > lo || __ballot(pv < 0) != 0;
+    const bool masked = tok + 64 > lo || (ONE ? pv < 0 : __ballot(pv < 0) != 0);
     f32x4 sc[NC][4];
 #pragma unroll
     for (int cc = 0; cc < ND; ++cc)
@@ -308,28 +362,28 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cac
           }
       }
 
+    // where there is no page its scale, which may be anything, is none
+    ks = pv < 0 ? 1.f : ks * a.scale;
+    vs = pv < 0 ? 0.f : vs;
     bf16x8 wf[NC][2][WP];
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-      float top = -INFINITY;
+      if (masked) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float y = sc[n][u][r] * ks;
-          if (masked) {
+          for (int r = 0; r < 4; ++r) {
             const bool ok = vt + u * 4 + r < lim[n] && pv >= 0;
-            y = ok ? y : -INFINITY;
+            sc[n][u][r] = ok ? sc[n][u][r] : -INFINITY;
             seen[n] |= ok;
           }
-          sc[n][u][r] = y;
-          top = fmaxf(top, y);
-        }
-      if (!masked) seen[n] = true;
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      top = fmaxf(top, m[n]);
-      const float base = top == -INFINITY ? 0.f : top;
+      } else {
+        seen[n] = true;
+      }
+      float best = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) best = max3(max3(best, sc[n][u][0], sc[n][u][1]), sc[n][u][2], sc[n][u][3]);
+      const float top = fmaxf(max_of_column(best * ks), m[n]), base = top == -INFINITY ? 0.f : top;
       if (__ballot(top > m[n])) {
         const float f = __builtin_amdgcn_exp2f(m[n] - base);
         l[n] *= f;
@@ -342,7 +396,7 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cac
         float p[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(sc[n][2 * half + e / 4][e % 4] - base);
+          p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][2 * half + e / 4][e % 4], ks, -base));
           l[n] += p[e];
           p[e] *= vs;
         }
@@ -352,7 +406,7 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cac
 
     if (masked) {
       // what stands behind the last visible token, or in no page, is not read as a number
-      const int left = hi - vt;
+      const int left = pv < 0 ? 0 : hi - vt;
       unsigned keep[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -374,7 +428,7 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cac
 #pragma unroll
           for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) see[n][half][e] = (bf16_t)(vt + half * 8 + e < lim[n] && pv >= 0 ? 1.f : 0.f);
+            for (int e = 0; e < 8; ++e) see[n][half][e] = (bf16_t)(vt + half * 8 + e < lim[n] ? 1.f : 0.f);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
           const unsigned b[4] = {nan_bytes(vr[j].x), nan_bytes(vr[j].y), nan_bytes(vr[j].z), nan_bytes(vr[j].w)};
@@ -394,7 +448,6 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cac
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      if (j * 16 >= dh) continue;
       const bf16x8 v0 = codes8(vr[j].x, vr[j].y), v1 = codes8(vr[j].z, vr[j].w);
 #pragma unroll
       for (int n = 0; n < NC; ++n)
@@ -410,7 +463,8 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cac
     if (tile + W < last) attend(tile + W, two, one);
   }
 
-  // the four lanes of a column, then the waves, two by two
+  // the four lanes of a column, then all waves at once: a thread has four columns of the head of one row
+  __syncthreads();                       // the queries have been read
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
     l[n] += __shfl_xor(l[n], 16, 64);
@@ -419,40 +473,43 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cac
     any |= __shfl_xor(any, 16, 64);
     any |= __shfl_xor(any, 32, 64);
     if (any && m[n] == -INFINITY && l[n] == 0.f) l[n] = -1.f;
-    for (int step = W / 2; step > 0; step >>= 1) {
-      __syncthreads();
-      if (wave >= step && wave < 2 * step) {
-        if (g == 0) { sml[wave - step][0][i] = m[n]; sml[wave - step][1][i] = l[n]; }
+    if (col0 + n * 16 + i >= columns) continue;
+    if (g == 0) sml[wave][n * 16 + i] = make_float2(m[n], l[n]);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4*>(&so[wave - step][i][j * 16 + g * 4]) = acc[n][j];
-      }
-      __syncthreads();
-      if (wave < step) {
-        const float m2 = sml[wave][0][i], l2 = sml[wave][1][i], top = fmaxf(m[n], m2), base = top == -INFINITY ? 0.f : top;
-        const float f = __builtin_amdgcn_exp2f(m[n] - base), f2 = __builtin_amdgcn_exp2f(m2 - base);
-        if (top == -INFINITY) l[n] = l[n] < 0.f || l2 < 0.f ? -1.f : l[n] + l2;       // nothing but minus infinities (or NaN) so far
-        else l[n] = (l[n] < 0.f ? 0.f : l[n] * f) + (l2 < 0.f ? 0.f : l2 * f2);
-        m[n] = top;
+    for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4*>(&so[wave][n * 16 + i][j * 16 + g * 4]) = acc[n][j];
+  }
+  __syncthreads();
+  const int quads = dh / 4, there = columns - col0 < width ? columns - col0 : width;
+  for (int it = threadIdx.x; it < there * quads; it += 64 * W) {
+    const int n = it / quads, d = (it - n * quads) * 4;
+    float2 ml[W];
+    float top = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[n][j] = acc[n][j] * f + *reinterpret_cast<const f32x4*>(&so[wave][i][j * 16 + g * 4]) * f2;
-      }
+    for (int v = 0; v < W; ++v) {
+      ml[v] = sml[v][n];
+      top = fmaxf(top, ml[v].x);
     }
-    if (wave != 0) continue;
-    const Column col = column_of(s, a, w.h, col0 + n * 16 + i);
-    if (!col.there) continue;
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    bool none = false;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < W; ++v) {
+      const float f = __builtin_amdgcn_exp2f(ml[v].x - base);
+      none |= ml[v].y < 0.f;
+      sum += ml[v].y < 0.f ? 0.f : top == -INFINITY ? ml[v].y : ml[v].y * f;        // minus infinity: no scores but such (or NaN)
+      o += *reinterpret_cast<const f32x4*>(&so[v][n][d]) * f;
+    }
+    if (none && top == -INFINITY && sum == 0.f) sum = -1.f;
     if (w.pieces > 1) {
       float* out = a.part + piece_at(c.B * c.Hkv * a.tiles, width, dh, w.slot);
-      if (g == 0) *reinterpret_cast<float2*>(out + width * dh + (n * 16 + i) * 2) = make_float2(m[n], l[n]);
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        if (j * 16 < dh) *reinterpret_cast<f32x4*>(out + (n * 16 + i) * dh + j * 16 + g * 4) = acc[n][j];
+      if (d == 0) *reinterpret_cast<float2*>(out + width * dh + n * 2) = make_float2(top, sum);
+      *reinterpret_cast<f32x4*>(out + n * dh + d) = o;
     } else {
-      const float f = over(m[n], l[n]);
-      T* out = (T*)a.o + col.row * a.ldo + col.head * dh;
-      if (a.lse && g == 0) a.lse[col.row * a.H + col.head] = log_sum(m[n], l[n]);
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        if (j * 16 < dh) put4(out + j * 16 + g * 4, acc[n][j] * f, a.vec);
+      const int t = new_of(col0 + n), head = w.h * a.G + col0 + n - t * a.G;
+      const int64_t row = s.first + t;
+      if (a.lse && d == 0) a.lse[row * a.H + head] = log_sum(top, sum);
+      put4((T*)a.o + row * a.ldo + head * dh + d, o * over(top, sum), a.vec);
     }
   }
 }
@@ -490,13 +547,6 @@ __device__ __forceinline__ float both_max(float v) {
 
 constexpr int kRuns = 128;                 // of sixteen tokens, whose pages and scales are known to a block ahead of their tiles
 struct Runs { int64_t at[kRuns]; float ks[kRuns], lv[kRuns], rv[kRuns]; };       // at: tokens of the pool before the run's, negative: no page
-// The largest of three; NaN count only where there is nothing else.  (As an instruction of its own: in C each operand would be made quiet first.)
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
-
 // NB: head size in units of 32 columns, rounded up; CG: column groups of 32 of a wave.
 template <typename T, int NB>
 __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
@@ -826,10 +876,10 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
 // The pieces of a divided axis, in their order.  A column belongs to a wave, or to the four of a block; a quad of its columns of the head to one lane
 // for every so many pieces.
 template <typename T, int WAVES>
-__global__ void __launch_bounds__(256) k_cache_join(CacheView c, AttnArgs a, int width) {
+__global__ void __launch_bounds__(256) k_cache_join(CacheView c, AttnArgs a, int width, unsigned groups) {
   __shared__ f32x4 sh[4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), dh = c.dh;
-  const unsigned id = blockIdx.y * gridDim.x + blockIdx.x, groups = width * WAVES / 4, pair = id / groups, pairs = c.B * c.Hkv * a.tiles;
+  const unsigned id = blockIdx.y * gridDim.x + blockIdx.x, pair = id / groups, pairs = c.B * c.Hkv * a.tiles;
   if (pair >= pairs) return;
   const int n = (int)(id - pair * groups) * (4 / WAVES) + (WAVES == 4 ? 0 : wave);
   const int tile = (int)(pair % a.tiles), h = (int)(pair / a.tiles % c.Hkv), b = (int)(pair / a.tiles / c.Hkv);
@@ -896,7 +946,7 @@ Shape shape_of(int B, int T, int H, int Hkv, int dh, int64_t tokens) {
   s.tiles = (int)((columns + s.width - 1) / s.width);
   const int64_t pairs = (int64_t)B * Hkv * s.tiles, longest = (tokens + 63) / 64;
   s.waves = kWaves;
-  s.target = s.prompt ? 512 : 1024;
+  s.target = s.prompt ? 512 : 512;
   if (!s.prompt && s.nc == 1 && dh <= 128 && longest <= 32 && pairs <= 256) {
     s.waves = 8;
     s.target = 0;
@@ -935,7 +985,7 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
   const size_t need = cache_attn_scratch(view.B, view.T, H, view.Hkv, dh, page, view.max_pages);
   if (need && (!c.partial || c.partial_elems < need || ((uintptr_t)c.partial & 15))) return hipErrorInvalidValue;
   const int G = H / view.Hkv;
-  AttnArgs a{q, o, lse, c.partial, ldq, ldo, H, G, causal != 0, s.tiles, s.target,
+  AttnArgs a{q, o, lse, c.partial, ldq, ldo, H, G, causal != 0, s.tiles, (unsigned)((((uint64_t)1 << 32) + G - 1) / G), s.target,
              ldq % 8 == 0 && ldo % 8 == 0 && (((uintptr_t)q | (uintptr_t)o) & 15) == 0, kLog2e / sqrtf((float)dh)};
   const int64_t pairs = (int64_t)view.B * view.Hkv * s.tiles;
   auto grid = [](int64_t blocks) {
@@ -948,8 +998,9 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
     typedef decltype(t) T;
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !s.target) return e;
-    if (s.prompt) k_cache_join<T, 1><<<grid(pairs * s.width / 4), 256, 0, c.stream>>>(view, a, s.width);
-    else k_cache_join<T, 4><<<grid(pairs * s.width), 256, 0, c.stream>>>(view, a, s.width);
+    const int most = view.T * G < s.width ? view.T * G : s.width;       // columns of a tile
+    if (s.prompt) k_cache_join<T, 1><<<grid(pairs * (s.width / 4)), 256, 0, c.stream>>>(view, a, s.width, s.width / 4);
+    else k_cache_join<T, 4><<<grid(pairs * most), 256, 0, c.stream>>>(view, a, s.width, most);
     return hipGetLastError();
   };
   auto go = [&](auto t, auto nd, auto nc) {
@@ -957,11 +1008,13 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
     constexpr int ND = decltype(nd)::value, NC = decltype(nc)::value;
     if constexpr (NC == 1 && ND <= 2) {
       if (s.waves == 8) {
-        k_cache_attn<T, ND, NC, 8><<<grid(pairs), 512, 0, c.stream>>>(view, a);
+        if (page >= 64) k_cache_attn<T, ND, NC, 8, true><<<grid(pairs), 512, 0, c.stream>>>(view, a);
+        else k_cache_attn<T, ND, NC, 8, false><<<grid(pairs), 512, 0, c.stream>>>(view, a);
         return join(t);
       }
     }
-    k_cache_attn<T, ND, NC, kWaves><<<grid(pairs + s.target), 64 * kWaves, 0, c.stream>>>(view, a);
+    if (page >= 64) k_cache_attn<T, ND, NC, kWaves, true><<<grid(pairs + s.target), 64 * kWaves, 0, c.stream>>>(view, a);
+    else k_cache_attn<T, ND, NC, kWaves, false><<<grid(pairs + s.target), 64 * kWaves, 0, c.stream>>>(view, a);
     return join(t);
   };
   auto many = [&](auto t, auto nb) {
