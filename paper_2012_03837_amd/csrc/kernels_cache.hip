@@ -2,9 +2,9 @@
 //   append:  s' = max(s of the page's earlier tokens, the least power of two with max |x| / s' <= 448),  code = e4m3(x / s'); where s' > s
 //            the page's earlier codes c become e4m3(c s / s')
 //   read:    x = code s
-// Bound by memory: one byte for every two or four.  A wave has a page, a head and a side (keys or values): an item of a lane is eight columns
-// of sixteen tokens, so that both sides are read as they stand in the rows, and written as they stand in the page: eight bytes a token of the keys, sixteen
-// a column of the values, transposed on the way in the lane's registers.
+// Bound by memory: one byte for every two or four.  A lane has eight columns of a run of sixteen tokens, so that both sides are read as they
+// stand in the rows, and written as they stand in the page: eight bytes a token of the keys, sixteen a column of the values, transposed on the way in the
+// lane's registers.
 #include <type_traits>
 
 #include "cache.h"
@@ -59,72 +59,178 @@ __device__ __forceinline__ unsigned rescale4(unsigned w, float ratio) {
   return pack4(v[0] * ratio, v[1] * ratio, v[2] * ratio, v[3] * ratio);
 }
 
-// What a wave works on: slot `slot` of sequence b holds the new rows row .. row + hi - lo - 1 at its tokens lo .. hi - 1.
-struct Part { int page, h, lo, hi; int64_t row; };
-__device__ __forceinline__ bool part_of(const CacheView& c, int64_t unit, int slots, Part* p) {
-  const int h = (int)(unit % c.Hkv);
-  const int64_t rest = unit / c.Hkv;
-  const int b = (int)(rest / slots);
-  if (b >= c.B) return false;
+// Slot `slot` of a sequence holds the new rows row .. row + hi - lo - 1 at its tokens lo .. hi - 1.
+struct Part { int page, lo, hi; int64_t row; };
+__device__ __forceinline__ bool part_of(const CacheView& c, int b, int nth, Part* p) {
   const Sequence s = sequence_of(c, b);
-  const int from = s.len - s.n, slot = (from >> c.shift) + (int)(rest % slots);      // from < 0: there is no page for those rows
+  const int from = s.len - s.n, slot = (from >> c.shift) + nth;      // from < 0: there is no page for those rows
   const int64_t base = (int64_t)slot << c.shift;
   const int64_t lo = from > base ? from - base : 0, end = s.len - base;
   p->lo = (int)lo;
   p->hi = (int)(end < ((int64_t)1 << c.shift) ? end : (int64_t)1 << c.shift);
   p->row = s.first + (base + lo - from);
-  p->h = h;
   if (p->hi <= p->lo) return false;
   p->page = page_of(c, b, slot);
   return true;
 }
+// The largest number of the `lanes` (a power of two) lanes of a head.
+__device__ __forceinline__ float max_of_head(float v, int lanes) {
+  for (int o = lanes >> 1; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ __forceinline__ float largest(const float (&v)[8], float most) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) most = finite(v[e]) ? fmaxf(most, fabsf(v[e])) : most;
+  return most;
+}
+// Eight columns (from d on) of a run's tokens that are there already, at a larger scale; tokens from `end` (of the page) on stay as they are.
+__device__ __forceinline__ void move_keys(uint8_t* pool, int dh, int d, int run, int end, float ratio) {
+  const int n = end - run * 16 < 16 ? end - run * 16 : 16;
+#pragma unroll 4
+  for (int t = 0; t < n; ++t) {
+    uint2* p = reinterpret_cast<uint2*>(pool + (run * 16 + t) * dh + d);
+    const uint2 w = *p;
+    *p = make_uint2(rescale4(w.x, ratio), rescale4(w.y, ratio));
+  }
+}
+__device__ __forceinline__ void move_values(uint8_t* pool, int size, int d, int run, int end, float ratio) {
+#pragma unroll 2
+  for (int e = 0; e < 8; ++e) {
+    uint4* p = reinterpret_cast<uint4*>(pool + (d + e) * size + run * 16);
+    const uint4 was = *p;
+    unsigned o[4] = {was.x, was.y, was.z, was.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int left = end - run * 16 - 4 * q;
+      const unsigned keep = left >= 4 ? 0u : left <= 0 ? 0xffffffffu : ~((1u << (8 * left)) - 1u);
+      o[q] = (rescale4(o[q], ratio) & ~keep) | (o[q] & keep);
+    }
+    *p = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+}
 
+// One new row a sequence: a wave has a side and as many heads as it has lanes for, eight columns a lane.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) k_cache_append(CacheView c, Rows<const T> x, int slots) {
-  const int lane = threadIdx.x & 63;
-  const int64_t unit = ((int64_t)(blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x) >> 6;
-  const bool values = unit & 1;
+__global__ void __launch_bounds__(256) k_cache_append_one(CacheView c, Rows<const T> x, int lanes, int groups) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned unit = (blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave, b = unit / (2 * groups), part = unit - b * 2 * groups;
+  if (b >= (unsigned)c.B) return;
+  const bool values = part >= (unsigned)groups;
+  const int h = (int)(values ? part - groups : part) * (64 / lanes) + lane / lanes, d = (lane & (lanes - 1)) * 8;
   Part p;
-  if (!part_of(c, unit >> 1, slots, &p) || p.page < 0) return;
-  const int cols = c.dh / 8, size = 1 << c.shift;
-  const T* rows = (values ? x.v + p.row * x.ldv : x.k + p.row * x.ldk) + p.h * c.dh;
-  const int64_t ld = values ? x.ldv : x.ldk, where = (int64_t)p.page * c.Hkv + p.h;
+  if (!part_of(c, b, 0, &p) || p.page < 0 || h >= c.Hkv) return;
+  const int size = 1 << c.shift;
+  const int64_t where = (int64_t)p.page * c.Hkv + h;
   float* scale = (values ? c.vs : c.ks) + where;
   uint8_t* pool = (values ? c.v : c.k) + (where * c.dh << c.shift);
-
-  const int first = p.lo >> 4, runs = ((p.hi + 15) >> 4) - first;
-  float most = 0.f;
-  for (int i = lane; i < runs * cols; i += 64) {
-    const int r = first + i / cols, d = (i % cols) * 8;
-#pragma unroll 4
-    for (int t = 0; t < 16; ++t) {
-      const int at = r * 16 + t;
-      if (at < p.lo || at >= p.hi) continue;
-      float v[8];
-      take8<T, VEC>(rows + (at - p.lo) * ld + d, v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) most = finite(v[e]) ? fmaxf(most, fabsf(v[e])) : most;
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  const float old = p.lo > 0 ? *scale : 0.f;
+  if (d < c.dh) take8<T, VEC>((values ? x.v + p.row * x.ldv : x.k + p.row * x.ldk) + h * c.dh + d, v);
+  const float need = scale_for(max_of_head(largest(v, 0.f), lanes)), s = old > need ? old : need, inv = 1.f / s;
+  if (d >= c.dh) return;
+  if (d == 0) *scale = s;
+  if (p.lo > 0 && s > old) {
+    const float ratio = old / s;
+    for (int r = 0; r * 16 < p.lo; ++r) {
+      if (values) move_values(pool, size, d, r, p.lo, ratio);
+      else move_keys(pool, c.dh, d, r, p.lo, ratio);
     }
   }
+  const unsigned a = pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv), w = pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+  if (values) {
+    uint8_t* to = pool + d * size + p.lo;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+    for (int e = 0; e < 8; ++e) to[e * size] = (uint8_t)((e < 4 ? a : w) >> (8 * (e % 4)));
+  } else {
+    *reinterpret_cast<uint2*>(pool + p.lo * c.dh + d) = make_uint2(a, w);
+  }
+}
+
+// Several: a block has a page, a side and the heads that its 64 lanes have room for; a wave has every fourth run of sixteen tokens.  So rows are read
+// in stretches of some heads, and what a page and head takes is found in one pass over LDS.  KEEP: pages of at most four runs, whose rows stay in registers between
+// the largest number and the codes; otherwise they are read twice.
+template <typename T, bool VEC, bool KEEP>
+__global__ void __launch_bounds__(256) k_cache_append(CacheView c, Rows<const T> x, int lanes, int groups, int slots) {
+  typedef __attribute__((ext_vector_type(8))) T Raw;
+  __shared__ float found[4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned unit = blockIdx.y * gridDim.x + blockIdx.x, rest = unit / (2 * groups), part = unit - rest * 2 * groups, b = rest / slots;
+  if (b >= (unsigned)c.B) return;
+  const bool values = part >= (unsigned)groups;
+  const int h = (int)(values ? part - groups : part) * (64 / lanes) + lane / lanes, d = (lane & (lanes - 1)) * 8;
+  Part p;
+  if (!part_of(c, b, rest - b * slots, &p) || p.page < 0) return;
+  const bool there = h < c.Hkv && d < c.dh;
+  const int size = 1 << c.shift;
+  const int64_t where = (int64_t)p.page * c.Hkv + (there ? h : 0);
+  float* scale = (values ? c.vs : c.ks) + where;
+  uint8_t* pool = (values ? c.v : c.k) + (where * c.dh << c.shift);
+  const T* rows = (values ? x.v + p.row * x.ldv : x.k + p.row * x.ldk) + h * c.dh + d;
+  const int64_t ld = values ? x.ldv : x.ldk;
   const float old = p.lo > 0 ? *scale : 0.f;
+
+  Raw raw[KEEP ? 16 : 1];
+  auto token = [&](int at, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    if (there && at >= p.lo && at < p.hi) take8<T, VEC>(rows + (at - p.lo) * ld, v);
+  };
+  float most = 0.f;
+  if constexpr (KEEP) {
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+      const int at = wave * 16 + t;
+      raw[t] = Raw{};
+      if (there && at >= p.lo && at < p.hi) {
+        if constexpr (VEC) {
+          raw[t] = *reinterpret_cast<const Raw*>(rows + (at - p.lo) * ld);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) raw[t][e] = rows[(at - p.lo) * ld + e];
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = to_f(raw[t][e]);
+      most = largest(v, most);
+    }
+  } else {
+    for (int r = (p.lo >> 4) + wave; r * 16 < p.hi; r += 4)
+#pragma unroll 4
+      for (int t = 0; t < 16; ++t) {
+        float v[8];
+        token(r * 16 + t, v);
+        most = largest(v, most);
+      }
+  }
+  found[wave][lane] = max_of_head(most, lanes);
+  __syncthreads();
+  most = fmaxf(fmaxf(found[0][lane], found[1][lane]), fmaxf(found[2][lane], found[3][lane]));
   const float need = scale_for(most), s = old > need ? old : need, inv = 1.f / s;
+  if (!there) return;
+  if (wave == 0 && d == 0) *scale = s;                  // the old one has been read by all: it came before the barrier
   const bool grown = p.lo > 0 && s > old;
   const float ratio = old / s;
-  if (lane == 0) *scale = s;
-
-  const int from = grown ? 0 : first, all = ((p.hi + 15) >> 4) - from;
-  for (int i = lane; i < all * cols; i += 64) {
-    const int r = from + i / cols, d = (i % cols) * 8;
+  // runs by the same wave in both: what is there already moves first, then the new tokens come
+  for (int r = wave; r * 16 < p.hi; r += 4) {
+    if (grown && r * 16 < p.lo) {
+      if (values) move_values(pool, size, d, r, p.lo, ratio);
+      else move_keys(pool, c.dh, d, r, p.lo, ratio);
+    }
+    if (r * 16 + 16 <= p.lo) continue;
     unsigned code[16][2];                // [token][columns]
 #pragma unroll
     for (int t = 0; t < 16; ++t) {
-      const int at = r * 16 + t;
-      code[t][0] = code[t][1] = 0;
-      if (at < p.lo || at >= p.hi) continue;
       float v[8];
-      take8<T, VEC>(rows + (at - p.lo) * ld + d, v);
+      if constexpr (KEEP) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = to_f(raw[t][e]);
+      } else {
+        token(r * 16 + t, v);
+      }
       code[t][0] = pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
       code[t][1] = pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
     }
@@ -132,14 +238,7 @@ __global__ void __launch_bounds__(256) k_cache_append(CacheView c, Rows<const T>
 #pragma unroll
       for (int t = 0; t < 16; ++t) {
         const int at = r * 16 + t;
-        uint2* to = reinterpret_cast<uint2*>(pool + at * c.dh + d);
-        if (at < p.lo) {
-          if (!grown) continue;
-          const uint2 w = *to;
-          *to = make_uint2(rescale4(w.x, ratio), rescale4(w.y, ratio));
-        } else if (at < p.hi) {
-          *to = make_uint2(code[t][0], code[t][1]);
-        }
+        if (at >= p.lo && at < p.hi) *reinterpret_cast<uint2*>(pool + at * c.dh + d) = make_uint2(code[t][0], code[t][1]);
       }
       continue;
     }
@@ -149,27 +248,13 @@ __global__ void __launch_bounds__(256) k_cache_append(CacheView c, Rows<const T>
       uint8_t* to = pool + (d + e) * size + r * 16;
       unsigned w[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        w[q] = 0;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) w[q] |= (code[4 * q + t][e / 4] >> (8 * (e % 4)) & 0xffu) << (8 * t);
+      for (int q = 0; q < 4; ++q) {      // byte e % 4 of four tokens
+        const unsigned pick = 0x0c0c0400u + 0x0101u * (e % 4);
+        const unsigned lo = __builtin_amdgcn_perm(code[4 * q + 1][e / 4], code[4 * q][e / 4], pick);
+        const unsigned hi = __builtin_amdgcn_perm(code[4 * q + 3][e / 4], code[4 * q + 2][e / 4], pick);
+        w[q] = lo | hi << 16;
       }
       if (whole) {
-        *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-      } else if (grown) {
-        const uint4 was = *reinterpret_cast<const uint4*>(to);
-        const unsigned o[4] = {was.x, was.y, was.z, was.w};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const unsigned moved = rescale4(o[q], ratio);
-          unsigned out = 0;
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const int at = r * 16 + 4 * q + t;
-            out |= (at < p.lo ? moved : at < p.hi ? w[q] : o[q]) & 0xffu << (8 * t);
-          }
-          w[q] = out;
-        }
         *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
       } else {
 #pragma unroll
@@ -182,59 +267,57 @@ __global__ void __launch_bounds__(256) k_cache_append(CacheView c, Rows<const T>
   }
 }
 
+// The same blocks, waves and lanes.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) k_cache_read(CacheView c, Rows<T> x, int slots) {
-  const int lane = threadIdx.x & 63;
-  const int64_t unit = ((int64_t)(blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x) >> 6;
-  const bool values = unit & 1;
+__global__ void __launch_bounds__(256) k_cache_read(CacheView c, Rows<T> x, int lanes, int groups, int slots) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned unit = blockIdx.y * gridDim.x + blockIdx.x, rest = unit / (2 * groups), part = unit - rest * 2 * groups, b = rest / slots;
+  if (b >= (unsigned)c.B) return;
+  const bool values = part >= (unsigned)groups;
+  const int h = (int)(values ? part - groups : part) * (64 / lanes) + lane / lanes, d = (lane & (lanes - 1)) * 8;
   Part p;
-  if (!part_of(c, unit >> 1, slots, &p)) return;
-  const int cols = c.dh / 8, size = 1 << c.shift;
-  T* rows = (values ? x.v + p.row * x.ldv : x.k + p.row * x.ldk) + p.h * c.dh;
-  const int64_t ld = values ? x.ldv : x.ldk, where = (int64_t)p.page * c.Hkv + p.h;
-  const int first = p.lo >> 4, runs = ((p.hi + 15) >> 4) - first;
+  if (!part_of(c, b, rest - b * slots, &p) || h >= c.Hkv || d >= c.dh) return;
+  const int size = 1 << c.shift;
   const bool there = p.page >= 0;
-  const float s = there ? (values ? c.vs : c.ks)[where] : 0.f;
-  const uint8_t* pool = (values ? c.v : c.k) + (there ? where * c.dh << c.shift : 0);
-  for (int i = lane; i < runs * cols; i += 64) {
-    const int r = first + i / cols, d = (i % cols) * 8;
-    unsigned w[8][4];                    // values: [column][tokens]
-    if (values && there) {
+  const int64_t where = (int64_t)(there ? p.page : 0) * c.Hkv + h;
+  T* rows = (values ? x.v + p.row * x.ldv : x.k + p.row * x.ldk) + h * c.dh + d;
+  const int64_t ld = values ? x.ldv : x.ldk;
+  const float s = (values ? c.vs : c.ks)[where];
+  const uint8_t* pool = (values ? c.v : c.k) + (where * c.dh << c.shift);
+  for (int r = (p.lo >> 4) + wave; r * 16 < p.hi; r += 4) {
+    uint2 w[16];                         // [token]: eight columns
+    if (values) {
+      unsigned q[8][4];                  // [column]: sixteen tokens
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint4 q = *reinterpret_cast<const uint4*>(pool + (d + e) * size + r * 16);
-        w[e][0] = q.x; w[e][1] = q.y; w[e][2] = q.z; w[e][3] = q.w;
+        const uint4 f = *reinterpret_cast<const uint4*>(pool + (d + e) * size + r * 16);
+        q[e][0] = f.x; q[e][1] = f.y; q[e][2] = f.z; q[e][3] = f.w;
       }
+#pragma unroll
+      for (int t = 0; t < 16; ++t) {
+        const unsigned pick = 0x0c0c0400u + 0x0101u * (t % 4);
+        auto four = [&](int e) {
+          return __builtin_amdgcn_perm(q[e + 1][t / 4], q[e][t / 4], pick) | __builtin_amdgcn_perm(q[e + 3][t / 4], q[e + 2][t / 4], pick) << 16;
+        };
+        w[t] = make_uint2(four(0), four(4));
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 16; ++t) w[t] = *reinterpret_cast<const uint2*>(pool + (r * 16 + t) * c.dh + d);
     }
 #pragma unroll
     for (int t = 0; t < 16; ++t) {
       const int at = r * 16 + t;
       if (at < p.lo || at >= p.hi) continue;
-      float v[8];
-      if (!there) {
+      float f[4], g[4], v[8];
+      unpack4(w[t].x, f);
+      unpack4(w[t].y, g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.f;
-      } else {
-        unsigned a, b;
-        if (values) {
-          a = b = 0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            a |= (w[e][t / 4] >> (8 * (t % 4)) & 0xffu) << (8 * e);
-            b |= (w[4 + e][t / 4] >> (8 * (t % 4)) & 0xffu) << (8 * e);
-          }
-        } else {
-          const uint2 q = *reinterpret_cast<const uint2*>(pool + at * c.dh + d);
-          a = q.x;
-          b = q.y;
-        }
-        float f[4], g[4];
-        unpack4(a, f);
-        unpack4(b, g);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { v[e] = f[e] * s; v[4 + e] = g[e] * s; }
+      for (int e = 0; e < 4; ++e) {
+        v[e] = there ? f[e] * s : 0.f;
+        v[4 + e] = there ? g[e] * s : 0.f;
       }
-      put8<T, VEC>(rows + (at - p.lo) * ld + d, v);
+      put8<T, VEC>(rows + (at - p.lo) * ld, v);
     }
   }
 }
@@ -254,19 +337,21 @@ bool cache_operands_ok(const CacheView& c) {
 }
 
 namespace {
+// Lanes of a head, groups of heads, slots of a sequence that new rows may stand in, and the grid of `units` a group, side and slot to a block.
 template <typename T, typename F>
-hipError_t by_unit(const CacheView& c, const void* k, int64_t ldk, const void* v, int64_t ldv, F&& launch) {
+hipError_t by_unit(const CacheView& c, const void* k, int64_t ldk, const void* v, int64_t ldv, int units, F&& launch) {
   const int64_t width = (int64_t)c.Hkv * c.dh, widest = (int64_t)1 << 32;
   if (ldk < width || ldv < width || ldk > widest || ldv > widest) return hipErrorInvalidValue;
   if (c.B == 0 || c.rows == 0) return hipSuccess;
   if (!k || !v || !cache_operands_ok(c)) return hipErrorInvalidValue;
+  const int lanes = c.dh <= 16 ? 2 : c.dh <= 32 ? 4 : c.dh <= 64 ? 8 : c.dh <= 128 ? 16 : 32, heads = 64 / lanes, groups = (c.Hkv + heads - 1) / heads;
   const int slots = ((c.T + (1 << c.shift) - 2) >> c.shift) + 1;
-  const int64_t blocks = ((int64_t)c.B * slots * c.Hkv * 2 + 3) / 4;
+  const int64_t blocks = ((int64_t)c.B * slots * groups * 2 + units - 1) / units;
   constexpr int64_t most = 1 << 21;              // a launch has less than 2^32 threads along x
-  if (blocks > most * 1024) return hipErrorInvalidValue;
+  if (blocks * units > (int64_t)1 << 31) return hipErrorInvalidValue;
   const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)((blocks + most - 1) / most));
-  if (ldk % 8 == 0 && ldv % 8 == 0 && (((uintptr_t)k | (uintptr_t)v) & 15) == 0) launch(std::true_type(), grid, slots);
-  else launch(std::false_type(), grid, slots);
+  if (ldk % 8 == 0 && ldv % 8 == 0 && (((uintptr_t)k | (uintptr_t)v) & 15) == 0) launch(std::true_type(), grid, lanes, groups, slots);
+  else launch(std::false_type(), grid, lanes, groups, slots);
   return hipGetLastError();
 }
 }  // namespace
@@ -274,8 +359,12 @@ hipError_t by_unit(const CacheView& c, const void* k, int64_t ldk, const void* v
 hipError_t op_cache_append(const OpCtx& c, const CacheView& view, const void* k, int64_t ldk, const void* v, int64_t ldv) {
   auto go = [&](auto t) {
     typedef decltype(t) T;
-    return by_unit<T>(view, k, ldk, v, ldv, [&](auto vec, dim3 grid, int slots) {
-      k_cache_append<T, decltype(vec)::value><<<grid, 256, 0, c.stream>>>(view, Rows<const T>{(const T*)k, (const T*)v, ldk, ldv}, slots);
+    const Rows<const T> x{(const T*)k, (const T*)v, ldk, ldv};
+    return by_unit<T>(view, k, ldk, v, ldv, view.T == 1 ? 4 : 1, [&](auto vec, dim3 grid, int lanes, int groups, int slots) {
+      constexpr bool VEC = decltype(vec)::value;
+      if (view.T == 1) k_cache_append_one<T, VEC><<<grid, 256, 0, c.stream>>>(view, x, lanes, groups);
+      else if (view.shift <= 6) k_cache_append<T, VEC, true><<<grid, 256, 0, c.stream>>>(view, x, lanes, groups, slots);
+      else k_cache_append<T, VEC, false><<<grid, 256, 0, c.stream>>>(view, x, lanes, groups, slots);
     });
   };
   return c.dt == BF16 ? go(bf16_t()) : go(float());
@@ -284,8 +373,9 @@ hipError_t op_cache_append(const OpCtx& c, const CacheView& view, const void* k,
 hipError_t op_cache_read(const OpCtx& c, const CacheView& view, void* k, int64_t ldk, void* v, int64_t ldv) {
   auto go = [&](auto t) {
     typedef decltype(t) T;
-    return by_unit<T>(view, k, ldk, v, ldv, [&](auto vec, dim3 grid, int slots) {
-      k_cache_read<T, decltype(vec)::value><<<grid, 256, 0, c.stream>>>(view, Rows<T>{(T*)k, (T*)v, ldk, ldv}, slots);
+    const Rows<T> x{(T*)k, (T*)v, ldk, ldv};
+    return by_unit<T>(view, k, ldk, v, ldv, 1, [&](auto vec, dim3 grid, int lanes, int groups, int slots) {
+      k_cache_read<T, decltype(vec)::value><<<grid, 256, 0, c.stream>>>(view, x, lanes, groups, slots);
     });
   };
   return c.dt == BF16 ? go(bf16_t()) : go(float());
