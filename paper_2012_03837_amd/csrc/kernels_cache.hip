@@ -146,13 +146,13 @@ __global__ void __launch_bounds__(256) k_cache_append_one(CacheView c, Rows<cons
   }
 }
 
-// Several: a block has a page, a side and the heads that its 64 lanes have room for; a wave has every fourth run of sixteen tokens.  So rows are read
-// in stretches of some heads, and what a page and head takes is found in one pass over LDS.  KEEP: pages of at most four runs, whose rows stay in registers between
+// Several: a block has a page, a side and the heads that its 64 lanes have room for; a wave of W has every W-th run of sixteen tokens.  So rows are read
+// in stretches of some heads, and what a page and head takes is found in one pass over LDS.  KEEP: pages of at most W runs, whose rows stay in registers between
 // the largest number and the codes; otherwise they are read twice.
-template <typename T, bool VEC, bool KEEP>
-__global__ void __launch_bounds__(256) k_cache_append(CacheView c, Rows<const T> x, int lanes, int groups, int slots) {
+template <typename T, bool VEC, bool KEEP, int W>
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && KEEP ? 4 : 2) k_cache_append(CacheView c, Rows<const T> x, int lanes, int groups, int slots) {
   typedef __attribute__((ext_vector_type(8))) T Raw;
-  __shared__ float found[4][64];
+  __shared__ float found[W][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned unit = blockIdx.y * gridDim.x + blockIdx.x, rest = unit / (2 * groups), part = unit - rest * 2 * groups, b = rest / slots;
   if (b >= (unsigned)c.B) return;
@@ -196,9 +196,10 @@ __global__ void __launch_bounds__(256) k_cache_append(CacheView c, Rows<const T>
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = to_f(raw[t][e]);
       most = largest(v, most);
+      if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);
     }
   } else {
-    for (int r = (p.lo >> 4) + wave; r * 16 < p.hi; r += 4)
+    for (int r = (p.lo >> 4) + wave; r * 16 < p.hi; r += W)
 #pragma unroll 4
       for (int t = 0; t < 16; ++t) {
         float v[8];
@@ -208,22 +209,31 @@ __global__ void __launch_bounds__(256) k_cache_append(CacheView c, Rows<const T>
   }
   found[wave][lane] = max_of_head(most, lanes);
   __syncthreads();
-  most = fmaxf(fmaxf(found[0][lane], found[1][lane]), fmaxf(found[2][lane], found[3][lane]));
+#pragma unroll
+  for (int q = 0; q < W; ++q) most = fmaxf(most, found[q][lane]);
   const float need = scale_for(most), s = old > need ? old : need, inv = 1.f / s;
   if (!there) return;
+  if constexpr (KEEP && sizeof(T) == 2) {
+    // the rows stay as they are stored: their numbers, twice the registers, are not kept from the pass before
+    typedef __attribute__((ext_vector_type(4))) unsigned U;
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+      U u = __builtin_bit_cast(U, raw[t]);
+      asm volatile("" : "+v"(u));
+      raw[t] = __builtin_bit_cast(Raw, u);
+    }
+  }
   if (wave == 0 && d == 0) *scale = s;                  // the old one has been read by all: it came before the barrier
   const bool grown = p.lo > 0 && s > old;
   const float ratio = old / s;
   // runs by the same wave in both: what is there already moves first, then the new tokens come
-  for (int r = wave; r * 16 < p.hi; r += 4) {
+  auto write = [&](int r) {
     if (grown && r * 16 < p.lo) {
       if (values) move_values(pool, size, d, r, p.lo, ratio);
       else move_keys(pool, c.dh, d, r, p.lo, ratio);
     }
-    if (r * 16 + 16 <= p.lo) continue;
-    unsigned code[16][2];                // [token][columns]
-#pragma unroll
-    for (int t = 0; t < 16; ++t) {
+    if (r * 16 + 16 <= p.lo) return;
+    auto coded = [&](int t) {            // eight columns of a token
       float v[8];
       if constexpr (KEEP) {
 #pragma unroll
@@ -231,39 +241,46 @@ __global__ void __launch_bounds__(256) k_cache_append(CacheView c, Rows<const T>
       } else {
         token(r * 16 + t, v);
       }
-      code[t][0] = pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-      code[t][1] = pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
-    }
+      return make_uint2(pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv), pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
+    };
     if (!values) {
 #pragma unroll
       for (int t = 0; t < 16; ++t) {
         const int at = r * 16 + t;
-        if (at >= p.lo && at < p.hi) *reinterpret_cast<uint2*>(pool + at * c.dh + d) = make_uint2(code[t][0], code[t][1]);
+        if (at >= p.lo && at < p.hi) *reinterpret_cast<uint2*>(pool + at * c.dh + d) = coded(t);
       }
-      continue;
+      return;
+    }
+    unsigned w[8][4];                    // [column]: sixteen tokens
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint2 c0 = coded(4 * q), c1 = coded(4 * q + 1), c2 = coded(4 * q + 2), c3 = coded(4 * q + 3);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {      // byte e % 4 of four tokens
+        const unsigned pick = 0x0c0c0400u + 0x0101u * (e % 4);
+        w[e][q] = __builtin_amdgcn_perm(e < 4 ? c1.x : c1.y, e < 4 ? c0.x : c0.y, pick) | __builtin_amdgcn_perm(e < 4 ? c3.x : c3.y, e < 4 ? c2.x : c2.y, pick) << 16;
+      }
+      __builtin_amdgcn_sched_barrier(0);      // four tokens' numbers at a time in registers, not all sixteen's
     }
     const bool whole = r * 16 >= p.lo && r * 16 + 16 <= p.hi;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       uint8_t* to = pool + (d + e) * size + r * 16;
-      unsigned w[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {      // byte e % 4 of four tokens
-        const unsigned pick = 0x0c0c0400u + 0x0101u * (e % 4);
-        const unsigned lo = __builtin_amdgcn_perm(code[4 * q + 1][e / 4], code[4 * q][e / 4], pick);
-        const unsigned hi = __builtin_amdgcn_perm(code[4 * q + 3][e / 4], code[4 * q + 2][e / 4], pick);
-        w[q] = lo | hi << 16;
-      }
       if (whole) {
-        *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(to) = make_uint4(w[e][0], w[e][1], w[e][2], w[e][3]);
       } else {
 #pragma unroll
         for (int t = 0; t < 16; ++t) {
           const int at = r * 16 + t;
-          if (at >= p.lo && at < p.hi) to[t] = (uint8_t)(w[t / 4] >> (8 * (t % 4)));
+          if (at >= p.lo && at < p.hi) to[t] = (uint8_t)(w[e][t / 4] >> (8 * (t % 4)));
         }
       }
     }
+  };
+  if constexpr (KEEP) {                  // a wave has one run: no loop that numbers could be kept for
+    if (wave * 16 < p.hi) write(wave);
+  } else {
+    for (int r = wave + (grown ? 0 : p.lo / (16 * W) * W); r * 16 < p.hi; r += W) write(r);
   }
 }
 
@@ -363,8 +380,12 @@ hipError_t op_cache_append(const OpCtx& c, const CacheView& view, const void* k,
     return by_unit<T>(view, k, ldk, v, ldv, view.T == 1 ? 4 : 1, [&](auto vec, dim3 grid, int lanes, int groups, int slots) {
       constexpr bool VEC = decltype(vec)::value;
       if (view.T == 1) k_cache_append_one<T, VEC><<<grid, 256, 0, c.stream>>>(view, x, lanes, groups);
-      else if (view.shift <= 6) k_cache_append<T, VEC, true><<<grid, 256, 0, c.stream>>>(view, x, lanes, groups, slots);
-      else k_cache_append<T, VEC, false><<<grid, 256, 0, c.stream>>>(view, x, lanes, groups, slots);
+      else if (view.shift == 4) k_cache_append<T, VEC, true, 1><<<grid, 64, 0, c.stream>>>(view, x, lanes, groups, slots);
+      else if (view.shift == 5) k_cache_append<T, VEC, true, 2><<<grid, 128, 0, c.stream>>>(view, x, lanes, groups, slots);
+      else if (view.shift == 6) k_cache_append<T, VEC, true, 4><<<grid, 256, 0, c.stream>>>(view, x, lanes, groups, slots);
+      else if (view.shift == 7) k_cache_append<T, VEC, true, 8><<<grid, 512, 0, c.stream>>>(view, x, lanes, groups, slots);
+      else if constexpr (std::is_same<T, bf16_t>::value) k_cache_append<T, VEC, true, 16><<<grid, 1024, 0, c.stream>>>(view, x, lanes, groups, slots);
+      else k_cache_append<T, VEC, false, 8><<<grid, 512, 0, c.stream>>>(view, x, lanes, groups, slots);      // 128 registers do not hold sixteen rows in fp32
     });
   };
   return c.dt == BF16 ? go(bf16_t()) : go(float());
