@@ -41,14 +41,12 @@ __device__ __forceinline__ float scale_for(float most) {
   return __builtin_bit_cast(float, (unsigned)(e < 1 ? 1 : e) << 23);
 }
 __device__ __forceinline__ bool finite(float v) { return (__builtin_bit_cast(unsigned, v) & 0x7f800000u) != 0x7f800000u; }
-// An infinity has no code: it is held as a NaN.
-__device__ __forceinline__ unsigned pack2(float a, float b, unsigned w, bool high) {
-  const float nan = __builtin_bit_cast(float, 0x7fc00000u);
-  a = finite(a) ? a : nan;
-  b = finite(b) ? b : nan;
-  return high ? __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, true) : __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
+// Codes of finite numbers and NaN.
+__device__ __forceinline__ unsigned pack4(float a, float b, float c, float d) {
+  return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
-__device__ __forceinline__ unsigned pack4(float a, float b, float c, float d) { return pack2(c, d, pack2(a, b, 0, false), true); }
+// An infinity has no code: it is held as a NaN.
+__device__ __forceinline__ float coded(float v) { return finite(v) ? v : __builtin_bit_cast(float, 0x7fc00000u); }
 __device__ __forceinline__ void unpack4(unsigned w, float (&v)[4]) {
   const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
   v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1];
@@ -73,10 +71,41 @@ __device__ __forceinline__ bool part_of(const CacheView& c, int b, int nth, Part
   p->page = page_of(c, b, slot);
   return true;
 }
+// The larger of two numbers that are not negative; a NaN is larger than all.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_bit_cast(unsigned, a) > __builtin_bit_cast(unsigned, b) ? a : b; }
 // The largest number of the `lanes` (a power of two) lanes of a head.
 __device__ __forceinline__ float max_of_head(float v, int lanes) {
-  for (int o = lanes >> 1; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  for (int o = lanes >> 1; o > 0; o >>= 1) v = larger(v, __shfl_xor(v, o, 64));
   return v;
+}
+// Absolute values compare as whole numbers do; those of infinities and NaN are kInfinite and more.
+constexpr unsigned kInfinite = 0x7f800000u;
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+__device__ __forceinline__ unsigned largest_bits(const bf16x8& v, unsigned most) {         // most: two halves, each with the largest of every second number
+  const u32x4 w = __builtin_bit_cast(u32x4, v);
+  u16x2 m = __builtin_bit_cast(u16x2, most);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const unsigned u = w[e] & 0x7fff7fffu;
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, u));
+  }
+  return __builtin_bit_cast(unsigned, m);
+}
+__device__ __forceinline__ unsigned largest_bits(const f32x8& v, unsigned most) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float f = v[e];
+    const unsigned u = __builtin_bit_cast(unsigned, f) & 0x7fffffffu;
+    most = u > most ? u : most;
+  }
+  return most;
+}
+template <typename T> __device__ __forceinline__ unsigned as_float_bits(unsigned most) {
+  if (sizeof(T) == 4) return most;
+  const unsigned a = most << 16, b = most & 0xffff0000u;
+  return a > b ? a : b;
 }
 __device__ __forceinline__ float largest(const float (&v)[8], float most) {
 #pragma unroll
@@ -136,7 +165,9 @@ __global__ void __launch_bounds__(256) k_cache_append_one(CacheView c, Rows<cons
       else move_keys(pool, c.dh, d, r, p.lo, ratio);
     }
   }
-  const unsigned a = pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv), w = pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = coded(v[e]) * inv;
+  const unsigned a = pack4(v[0], v[1], v[2], v[3]), w = pack4(v[4], v[5], v[6], v[7]);
   if (values) {
     uint8_t* to = pool + d * size + p.lo;
 #pragma unroll
@@ -170,47 +201,60 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && KEEP ? 4 : 2) k_cach
   const float old = p.lo > 0 ? *scale : 0.f;
 
   Raw raw[KEEP ? 16 : 1];
-  auto token = [&](int at, float (&v)[8]) {
+  auto read = [&](int at) {
+    Raw v = Raw{};
+    if (there && at >= p.lo && at < p.hi) {
+      if constexpr (VEC) {
+        v = *reinterpret_cast<const Raw*>(rows + (at - p.lo) * ld);
+      } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    if (there && at >= p.lo && at < p.hi) take8<T, VEC>(rows + (at - p.lo) * ld, v);
-  };
-  float most = 0.f;
-  if constexpr (KEEP) {
-#pragma unroll
-    for (int t = 0; t < 16; ++t) {
-      const int at = wave * 16 + t;
-      raw[t] = Raw{};
-      if (there && at >= p.lo && at < p.hi) {
-        if constexpr (VEC) {
-          raw[t] = *reinterpret_cast<const Raw*>(rows + (at - p.lo) * ld);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) raw[t][e] = rows[(at - p.lo) * ld + e];
-        }
+        for (int e = 0; e < 8; ++e) v[e] = rows[(at - p.lo) * ld + e];
       }
     }
+    return v;
+  };
+  unsigned bits = 0;
+  if constexpr (KEEP) {
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
-      float v[8];
+    for (int t = 0; t < 16; ++t) raw[t] = read(wave * 16 + t);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = to_f(raw[t][e]);
-      most = largest(v, most);
-      if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int t = 0; t < 16; ++t) bits = largest_bits(raw[t], bits);
   } else {
     for (int r = (p.lo >> 4) + wave; r * 16 < p.hi; r += W)
 #pragma unroll 4
+      for (int t = 0; t < 16; ++t) bits = largest_bits(read(r * 16 + t), bits);
+  }
+  found[wave][lane] = max_of_head(__builtin_bit_cast(float, as_float_bits<T>(bits)), lanes);
+  __syncthreads();
+  float most = 0.f;
+#pragma unroll
+  for (int q = 0; q < W; ++q) most = larger(most, found[q][lane]);
+  // with infinities or NaN among them (the same in all waves) the finite ones are looked through by themselves
+  const bool odd = __ballot(__builtin_bit_cast(unsigned, most) >= kInfinite) != 0;
+  if (odd) {
+    most = 0.f;
+    for (int r = (p.lo >> 4) / W * W + wave; r * 16 < p.hi; r += W)
+#pragma unroll 1
       for (int t = 0; t < 16; ++t) {
+        const Raw x = read(r * 16 + t);
         float v[8];
-        token(r * 16 + t, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = to_f(x[e]);
         most = largest(v, most);
       }
-  }
-  found[wave][lane] = max_of_head(most, lanes);
-  __syncthreads();
+    __syncthreads();
+    found[wave][lane] = max_of_head(most, lanes);
+    __syncthreads();
+    most = 0.f;
 #pragma unroll
-  for (int q = 0; q < W; ++q) most = fmaxf(most, found[q][lane]);
+    for (int q = 0; q < W; ++q) most = fmaxf(most, found[q][lane]);
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int t = 0; t < 16; ++t)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) raw[t][e] = from_f<T>(coded(to_f(raw[t][e])));
+    }
+  }
   const float need = scale_for(most), s = old > need ? old : need, inv = 1.f / s;
   if (!there) return;
   if constexpr (KEEP && sizeof(T) == 2) {
@@ -233,13 +277,16 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && KEEP ? 4 : 2) k_cach
       else move_keys(pool, c.dh, d, r, p.lo, ratio);
     }
     if (r * 16 + 16 <= p.lo) return;
-    auto coded = [&](int t) {            // eight columns of a token
+    auto codes = [&](int t) {            // eight columns of a token
+      Raw x;
+      if constexpr (KEEP) x = raw[t];
+      else x = read(r * 16 + t);
       float v[8];
-      if constexpr (KEEP) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = to_f(raw[t][e]);
-      } else {
-        token(r * 16 + t, v);
+      for (int e = 0; e < 8; ++e) v[e] = to_f(x[e]);
+      if constexpr (!KEEP) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = coded(v[e]);
       }
       return make_uint2(pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv), pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
     };
@@ -247,14 +294,14 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && KEEP ? 4 : 2) k_cach
 #pragma unroll
       for (int t = 0; t < 16; ++t) {
         const int at = r * 16 + t;
-        if (at >= p.lo && at < p.hi) *reinterpret_cast<uint2*>(pool + at * c.dh + d) = coded(t);
+        if (at >= p.lo && at < p.hi) *reinterpret_cast<uint2*>(pool + at * c.dh + d) = codes(t);
       }
       return;
     }
     unsigned w[8][4];                    // [column]: sixteen tokens
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const uint2 c0 = coded(4 * q), c1 = coded(4 * q + 1), c2 = coded(4 * q + 2), c3 = coded(4 * q + 3);
+      const uint2 c0 = codes(4 * q), c1 = codes(4 * q + 1), c2 = codes(4 * q + 2), c3 = codes(4 * q + 3);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {      // byte e % 4 of four tokens
         const unsigned pick = 0x0c0c0400u + 0x0101u * (e % 4);
