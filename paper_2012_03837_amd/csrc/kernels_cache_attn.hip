@@ -546,7 +546,8 @@ __device__ __forceinline__ float both_max(float v) {
 }
 
 constexpr int kRuns = 128;                 // of sixteen tokens, whose pages and scales are known to a block ahead of their tiles
-struct Runs { int64_t at[kRuns]; float ks[kRuns], lv[kRuns], rv[kRuns]; };       // at: tokens of the pool before the run's, negative: no page
+// k, v: bytes of the pools before the run's in the block's head (where there is no page, those of page 0).
+struct Runs { int64_t k[kRuns], v[kRuns]; int here[kRuns]; float ks[kRuns], lv[kRuns], rv[kRuns]; };
 // NB: head size in units of 32 columns, rounded up; CG: column groups of 32 of a wave.
 template <typename T, int NB>
 __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
@@ -590,6 +591,7 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
   tiles_of((((a.target ? s.len : bhi) + 63) >> 6), w.piece, w.pieces, &tile, &last);
   if (last > (bhi + 63) >> 6) last = (bhi + 63) >> 6;
 
+  const int64_t page_bytes = (int64_t)c.Hkv * dh << c.shift;
   // 32 tiles' runs from tile t on; the two sets take turns
   auto known = [&](int t) -> Runs& { return runs[(t - tile) >> 5 & 1]; };
   auto look_up = [&](int t) {
@@ -598,7 +600,9 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
     const int64_t where = (int64_t)(p < 0 ? 0 : p) * c.Hkv + w.h;
     const float vs = p < 0 ? 1.f : c.vs[where];
     Runs& r = known(t);
-    r.at[tid] = p < 0 ? -1 : (((int64_t)p * c.Hkv) << c.shift) + (at & (page - 1));
+    r.k[tid] = (p < 0 ? 0 : p) * page_bytes + (at & (page - 1)) * dh;
+    r.v[tid] = (p < 0 ? 0 : p) * page_bytes + (at & (page - 1));
+    r.here[tid] = p < 0 ? 0 : -1;
     r.ks[tid] = p < 0 ? 1.f : c.ks[where] * a.scale;
     r.lv[tid] = __builtin_amdgcn_logf(vs);
     r.rv[tid] = 1.f / vs;
@@ -642,18 +646,16 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
       for (int v = 0; v < 16; ++v) acc[n][j][v] = 0.f;
   }
 
-  // A tile on its way: sixteen bytes of a token's keys, and of a column's values, a thread and load.  Of columns behind the head's, of tokens that nobody in the
-  // block sees and of pages that are not there, zeros.  A run's values start 16 columns times tokens behind its page's, its keys where its tokens do.
+  // A tile on its way: sixteen bytes of a token's keys, and of a column's values, a thread and load.  No load is skipped: where there is no page, page 0 is read
+  // and its scores and values are taken out; keys behind the head's columns are its last ones, against zeros of the query, and what comes of values there
+  // is not written.
   uint4 kr[kLoads], vr[kLoads];
   const uint8_t *kh[kLoads], *vh[kLoads];
-  bool kd[kLoads], vd[kLoads];
 #pragma unroll
   for (int u = 0; u < kLoads; ++u) {
-    const int x = tid + 256 * u, tok = x / (DH / 16), d = x % (DH / 16), e = x >> 2;
-    kd[u] = x < 64 * (DH / 16) && d * 16 < dh;
-    vd[u] = e < dh;
-    kh[u] = c.k + ((int64_t)w.h * dh << c.shift) + (tok & 15) * dh + d * 16;
-    vh[u] = c.v + (((int64_t)w.h * dh + e) << c.shift);
+    const int x = tid + 256 * u, tok = x / (DH / 16), d = x % (DH / 16) * 16, e = x >> 2;
+    kh[u] = c.k + ((int64_t)w.h * dh << c.shift) + (tok & 15) * dh + (d < dh ? d : dh - 16);
+    vh[u] = c.v + (((int64_t)w.h * dh + (e < dh ? e : dh - 1)) << c.shift);
   }
   auto fetch = [&](int t) {
     const Runs& r = known(t);
@@ -661,27 +663,28 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
       const int x = tid + 256 * u;
-      kr[u] = vr[u] = make_uint4(0, 0, 0, 0);
-      const int64_t ka = kd[u] ? r.at[run0 + (x / (DH / 16) >> 4)] : -1, va = vd[u] ? r.at[run0 + (x & 3)] : -1;
-      if (ka >= 0) kr[u] = *reinterpret_cast<const uint4*>(kh[u] + ka * dh);
-      if (va >= 0) vr[u] = *reinterpret_cast<const uint4*>(vh[u] + ((va & ~(int64_t)(page - 1)) * dh + (va & (page - 1))));
+      if (x >= 64 * (DH / 16)) continue;                   // whole waves
+      kr[u] = *reinterpret_cast<const uint4*>(kh[u] + r.k[run0 + (x / (DH / 16) >> 4)]);
+      vr[u] = *reinterpret_cast<const uint4*>(vh[u] + r.v[run0 + (x & 3)]);
     }
   };
   auto stage = [&](int t, int buf) {
-    const bool part = t * 64 + 64 > blo;
+    const Runs& kn = known(t);
+    const int run0 = (t - tile & 31) * 4;
+    const int4 here = *reinterpret_cast<const int4*>(&kn.here[run0]);
+    const bool part = t * 64 + 64 > blo || (here.x & here.y & here.z & here.w) == 0;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
       const int x = tid + 256 * u, tok = x / (DH / 16), d = x % (DH / 16);
-      if (x < 64 * (DH / 16)) {
-        *reinterpret_cast<bf16x8*>(&sk[buf][tok][d * 16]) = codes8(kr[u].x, kr[u].y);
-        *reinterpret_cast<bf16x8*>(&sk[buf][tok][d * 16 + 8]) = codes8(kr[u].z, kr[u].w);
-      }
+      if (x >= 64 * (DH / 16)) continue;
+      *reinterpret_cast<bf16x8*>(&sk[buf][tok][d * 16]) = codes8(kr[u].x, kr[u].y);
+      *reinterpret_cast<bf16x8*>(&sk[buf][tok][d * 16 + 8]) = codes8(kr[u].z, kr[u].w);
       const int e = x >> 2, run = x & 3;
-      if (e < DH) {
+      {
         unsigned q[4] = {vr[u].x, vr[u].y, vr[u].z, vr[u].w};
         if (part) {
           // what stands behind the last visible token is no number; a NaN leaves the product, and is told to the columns that see it
-          const int left = bhi - (t * 64 + run * 16);
+          const int left = kn.here[run0 + run] ? bhi - (t * 64 + run * 16) : 0;
           unsigned bits = 0;
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
@@ -719,8 +722,8 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
       const int run0 = (t - tile & 31) * 4;
       const f32x4 ks = *reinterpret_cast<const f32x4*>(&kn.ks[run0]), lv = *reinterpret_cast<const f32x4*>(&kn.lv[run0]),
                   rv = *reinterpret_cast<const f32x4*>(&kn.rv[run0]);
-      const int64_t pages[4] = {kn.at[run0], kn.at[run0 + 1], kn.at[run0 + 2], kn.at[run0 + 3]};
-      const bool masked = tok + 64 > lo || (pages[0] | pages[1] | pages[2] | pages[3]) < 0;
+      const int4 pg = *reinterpret_cast<const int4*>(&kn.here[run0]);
+      const bool away = (pg.x & pg.y & pg.z & pg.w) == 0, masked = tok + 64 > lo || away;
       f32x16 sc[CG][2];
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
@@ -738,11 +741,12 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
 #pragma unroll
       for (int n = 0; n < CG; ++n) {
         if (masked) {
+          const int here[4] = {pg.x, pg.y, pg.z, pg.w};
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const bool ok = pages[r] >= 0 && tok + r * 16 + half * 8 + e < lim[n];
+              const bool ok = here[r] && tok + r * 16 + half * 8 + e < lim[n];
               sc[n][r >> 1][(r & 1) * 8 + e] = ok ? sc[n][r >> 1][(r & 1) * 8 + e] : -INFINITY;
               seen[n] |= ok;
             }
@@ -781,6 +785,7 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
 #pragma unroll
             for (int e = 0; e < 8; ++e) l[n] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][r >> 1][(r & 1) * 8 + e], ks[r], -base));
         }
+        const float count = lost ? 0.f : back;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float up = lv[r] + off;
@@ -790,7 +795,7 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
             p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][r >> 1][(r & 1) * 8 + e], ks[r], up));
             sum += p[e];
           }
-          l[n] = __builtin_fmaf(lost ? 0.f : sum, lost ? 0.f : back * rv[r], l[n]);
+          l[n] = __builtin_fmaf(sum, count * rv[r], l[n]);
 #pragma unroll
           for (int q = 0; q < WP; ++q)
 #pragma unroll
@@ -812,7 +817,7 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
             for (int q = WP - 1; q >= 0; --q) acc[n][j] = mma32(vf, wf[n][r][q], acc[n][j]);
         }
       }
-      if (tok + 64 > blo) {
+      if (tok + 64 > blo || away) {
         unsigned long long any = 0;
         for (int d = lane; d < DH; d += 64) any |= *reinterpret_cast<const unsigned long long*>(snan[buf][d]);
         if (__ballot(any != 0)) {
