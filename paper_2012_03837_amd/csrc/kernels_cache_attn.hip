@@ -548,6 +548,40 @@ __device__ __forceinline__ float both_max(float v) {
 constexpr int kRuns = 128;                 // of sixteen tokens, whose pages and scales are known to a block ahead of their tiles
 // k, v: bytes of the pools before the run's in the block's head (where there is no page, those of page 0).
 struct Runs { int64_t k[kRuns], v[kRuns]; int here[kRuns]; float ks[kRuns], lv[kRuns], rv[kRuns]; };
+// Where axes are whole: block `n` in the order of the column tiles' numbers, last tiles (the longest chains of a prompt) first, through the sequences that have
+// such a tile and their heads.  Numbered without gaps, so that whatever share of the blocks a compute unit gets, in turn as they come, is like the others' (8 prompts of 4096, 3584
+// .. 512, 12 heads, with a place kept for every sequence and tile: 141 to 196 us by how the places fell on the units).
+__device__ __forceinline__ bool find_longest(const CacheView& c, const AttnArgs& a, int width, int64_t n, Work* w) {
+  w->piece = w->slot = 0;
+  w->pieces = 1;
+  if (c.B > 64) {
+    const int pairs = c.B * c.Hkv, turn = (int)(n / pairs), pair = (int)(n - (int64_t)turn * pairs);
+    w->tile = a.tiles - 1 - turn;
+    w->b = pair / c.Hkv;
+    w->h = pair - w->b * c.Hkv;
+    return turn < a.tiles;
+  }
+  const int lane = threadIdx.x & 63;
+  const unsigned own = lane < c.B ? ((unsigned)sequence_of(c, lane).n * a.G + width - 1) / width : 0;
+  auto from = [&](unsigned t) {          // column tiles of a head from number t on
+    return (unsigned)__builtin_amdgcn_readlane((int)running_sum(own > t ? own - t : 0u), 63);
+  };
+  const unsigned unit = (unsigned)(n / c.Hkv);
+  w->h = (int)(n - (int64_t)unit * c.Hkv);
+  unsigned t = 0, end = a.tiles;
+  if (unit >= from(0)) return false;
+  while (end - t > 1) {
+    const unsigned mid = (t + end) / 2;
+    if (from(mid) > unit) t = mid;
+    else end = mid;
+  }
+  unsigned long long who = __ballot(own > t);
+  for (unsigned skip = unit - from(t + 1); skip; --skip) who &= who - 1;
+  w->tile = (int)t;
+  w->b = __builtin_ctzll(who);
+  return true;
+}
+
 // NB: head size in units of 32 columns, rounded up; CG: column groups of 32 of a wave.
 template <typename T, int NB>
 __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
@@ -565,15 +599,7 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
     if (!find_work(c, a, width, (unsigned)id, &w)) return;
     note_pieces(c, a, w);
   } else {
-    // the longest first; a head's column tiles in turn on the eight parts of the chip, so that sequences of different lengths load them alike
-    const int pairs = c.B * c.Hkv, turn = (int)(id / pairs);
-    if (turn >= a.tiles) return;
-    w.tile = a.tiles - 1 - turn;
-    const int pair = (int)((id + turn) % pairs);
-    w.b = pair / c.Hkv;
-    w.h = pair - w.b * c.Hkv;
-    w.piece = w.slot = 0;
-    w.pieces = 1;
+    if (!find_longest(c, a, width, id, &w)) return;
   }
   const Sequence s = sequence_of(c, w.b);
   const int col0 = w.tile * width, columns = s.n * a.G;
