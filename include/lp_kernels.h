@@ -170,7 +170,7 @@ int lpk_rotary_frequencies(double* freq, int rot, double base, double factor, do
  * Attention: o = softmax(q k^T dh^-1/2) v for the rows of q [rows, H * dh] (leading dimension ldq; H a multiple of Hkv, heads h G .. h G + G - 1 read
  * head h of the cache, G = H / Hkv), over the positions up to the row's own if `causal`, otherwise all of the sequence's.  o [rows, H * dh]; lse fp32 [rows, H]
  * (may be null) = log-sum-exp of the scaled scores.  A row that sees no token becomes zeros, its lse minus infinity.  What a row does not see does not
- * change it, a NaN there included.  q and o do not overlap.  scratch_dev: lpk_cache_attention_scratch floats (needs no device; may be 0), 16-byte aligned; contents
+ * change it, a NaN there included.  Scales are positive, as append leaves them.  q and o do not overlap.  scratch_dev: lpk_cache_attention_scratch floats (needs no device; may be 0), 16-byte aligned; contents
  * undefined on return, so that calls which share it are ordered. */
 int lpk_cache_append(int dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, int rows, const int32_t* starts, const int32_t* lens,
                      const int32_t* table, void* kpages, void* vpages, float* kscale, float* vscale, int B, int T, int Hkv, int dh, int page,

@@ -800,10 +800,10 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
           top[n] = tn;
         }
         const float base = m[n] == -INFINITY ? 0.f : m[n], off = kTop - (top[n] == -INFINITY ? 0.f : top[n]);
-        // the exponent by which a weight with its values' scale is apart from the weight: where it is so low that weights of some
-        // account would be lost, they take an exponential of their own
+        // the exponent by which a weight with its values' scale is apart from the weight: where that, or the way back by the scale, leaves the range of
+        // 32 bits, the weights take an exponential of their own
         const float apart = off + base, least = fminf(fminf(lv[0], lv[1]), fminf(lv[2], lv[3])) + apart;
-        const bool lost = __ballot(least < -100.f) != 0;
+        const bool lost = __ballot(least < -100.f || fabsf(apart) > 100.f) != 0;
         const float back = __builtin_amdgcn_exp2f(-apart);
         if (lost) {
 #pragma unroll
@@ -873,8 +873,10 @@ __global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cach
     if (any && m[n] == -INFINITY && l[n] == 0.f) l[n] = -1.f;
     const int at = first + n * 32 + i;
     const Column col = column_of(s, a, w.h, at);
-    // from the weights' reference to the scores'
-    const float back = top[n] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[n] - m[n] - kTop);
+    // from the weights' reference to the scores', in two steps of half the exponent: one may leave the range
+    const float back = top[n] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(0.5f * (top[n] - m[n] - kTop));
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[n][j] *= back;
     if (!col.there) continue;
     if (w.pieces > 1) {
       float* out = a.part + piece_at(c.B * c.Hkv * a.tiles, width, dh, w.slot);
@@ -969,15 +971,17 @@ struct Shape { bool prompt; int nc, waves, width, tiles, target; };
 Shape shape_of(int B, int T, int H, int Hkv, int dh, int64_t tokens) {
   Shape s;
   const int64_t columns = (int64_t)T * (H / Hkv);
-  const int most = dh <= 64 ? 4 : dh <= 128 ? 2 : 1;         // column tiles of 16 that registers hold
-  s.prompt = columns > 64;
-  s.nc = s.prompt ? 1 : columns <= 16 ? 1 : columns <= 32 ? 2 : 4;
-  if (s.nc > most) s.nc = most;
+  // More than 32 columns go through LDS: bf16, 16 sequences of 4000, 64 columns as four tiles of 16 or as half of one of 128: heads of 64 60 and 42 us, of 128 (as two by
+  // two) 52 and 36; 32 columns: 38 and 41, 34 and 36.
+  s.prompt = columns > 32;
+  s.nc = !s.prompt && columns > 16 && dh <= 128 ? 2 : 1;      // more registers than two tiles of wider heads take there are not
   s.width = s.prompt ? 128 : 16 * s.nc;
   s.tiles = (int)((columns + s.width - 1) / s.width);
   const int64_t pairs = (int64_t)B * Hkv * s.tiles, longest = (tokens + 63) / 64;
   s.waves = kWaves;
-  s.target = s.prompt ? 512 : 512;
+  // Two blocks a compute unit: 2 contexts of 131071, 4 heads of 64, 36 us with 512 pieces, 40 with 1024 and 55 with 4096; 192 ragged ones the same to 5 %.
+  s.target = 512;
+  // Few short axes: eight waves side by side and no second launch (one context of 1000, 12 heads of 64: 7.3 us; in pieces 9.9 and 6.0 for joining them).
   if (!s.prompt && s.nc == 1 && dh <= 128 && longest <= 32 && pairs <= 256) {
     s.waves = 8;
     s.target = 0;
@@ -1054,9 +1058,7 @@ hipError_t op_cache_attn(const OpCtx& c, const CacheView& view, const void* q, i
     return join(t);
   };
   auto by_columns = [&](auto t, auto nd) {
-    constexpr int ND = decltype(nd)::value;
-    if constexpr (ND == 1) if (s.nc == 4) return go(t, nd, std::integral_constant<int, 4>());
-    if constexpr (ND <= 2) if (s.nc == 2) return go(t, nd, std::integral_constant<int, 2>());
+    if constexpr (decltype(nd)::value <= 2) if (s.nc == 2) return go(t, nd, std::integral_constant<int, 2>());
     return go(t, nd, std::integral_constant<int, 1>());
   };
   auto by_head = [&](auto t) {
