@@ -164,7 +164,7 @@ int lpk_rotary_frequencies(double* freq, int rot, double base, double factor, do
  * Append quantises rows of k and v (compute dtype, Hkv * dh columns, leading dimensions ldk and ldv): per page and head s' = max(s, need), need the least power
  * of two (2^-126 at least) with |x| / need <= 448 for all new finite x, s the scale of the page's earlier tokens (positions before the new rows'; none: s' =
  * need); code = e4m3(x / s'), rounded to nearest even, and where s' > s the earlier codes become e4m3(code s / s').  A NaN or an infinity is held as
- * a NaN and has no part in the scale.  Two sequences of one call write to different pages.
+ * a NaN and has no part in the scale.  The pages that one call writes are all different.
  * Read writes code * s of the same rows to k and v (zeros for positions before the first).
  *
  * Attention: o = softmax(q k^T dh^-1/2) v for the rows of q [rows, H * dh] (leading dimension ldq; H a multiple of Hkv, heads h G .. h G + G - 1 read

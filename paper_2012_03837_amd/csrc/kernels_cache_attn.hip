@@ -195,7 +195,7 @@ __device__ __forceinline__ float max_of_column(float v) {
 // worked on, and the page number of the one after that; its values while its scores are computed.  Loads are never skipped: where there is no page, page 0
 // is read and its scores and values are taken out, and columns behind the head's repeat its last sixteen, against zeros of the query.
 template <typename T, int ND, int NC, int W, bool ONE>
-__global__ void __launch_bounds__(64 * W, ND * NC <= 2 && NC == 1 ? 2 : 1) k_cache_attn(CacheView c, AttnArgs a) {
+__global__ void __launch_bounds__(64 * W, ND * NC <= 2 ? 2 : 1) k_cache_attn(CacheView c, AttnArgs a) {
   constexpr int QP = std::is_same<T, float>::value ? 3 : 1, WP = std::is_same<T, float>::value ? 3 : 2, NJ = 4 * ND;
   constexpr int kPad = 64 * ND + 4, width = 16 * NC, kFrags = (NC * ND * 2 + W - 1) / W;
   // the queries, and when the axis is done what waves hand to each other
@@ -584,7 +584,7 @@ __device__ __forceinline__ bool find_longest(const CacheView& c, const AttnArgs&
 
 // NB: head size in units of 32 columns, rounded up; CG: column groups of 32 of a wave.
 template <typename T, int NB>
-__global__ void __launch_bounds__(256, NB <= 4 && sizeof(T) == 2 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
+__global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
   constexpr bool F = std::is_same<T, float>::value;
   constexpr int CG = 1, QP = F ? 3 : 1, WP = F ? 2 : 1, DH = 32 * NB, KLD = DH + 8, VLD = 72, kLoads = (64 * (DH / 16) + 255) / 256;
   constexpr float kTop = 7.f, kLag = 8.f;
@@ -972,7 +972,7 @@ Shape shape_of(int B, int T, int H, int Hkv, int dh, int64_t tokens) {
   Shape s;
   const int64_t columns = (int64_t)T * (H / Hkv);
   // More than 32 columns go through LDS: bf16, 16 sequences of 4000, 64 columns as four tiles of 16 or as half of one of 128: heads of 64 60 and 42 us, of 128 (as two by
-  // two) 52 and 36; 32 columns: 38 and 41, 34 and 36.
+  // two) 52 and 36; 32 columns: 30 and 41, 34 and 36.
   s.prompt = columns > 32;
   s.nc = !s.prompt && columns > 16 && dh <= 128 ? 2 : 1;      // more registers than two tiles of wider heads take there are not
   s.width = s.prompt ? 128 : 16 * s.nc;
