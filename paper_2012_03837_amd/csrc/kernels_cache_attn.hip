@@ -65,12 +65,9 @@ __device__ __forceinline__ unsigned nan_bytes(unsigned w) {
   return (hit >> 7) * 0xffu;
 }
 
-// The largest of three; NaN count only where there is nothing else.  (As an instruction of its own: in C each operand would be made quiet first.)
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
+// The largest of three; NaN count only where there is nothing else.  In C, which becomes the instruction of that name: scores come straight from the matrix
+// unit, and the compiler sees to the wait states (8 behind a 16 x 16 x 32 product, 12 behind one of 32 x 32 x 16) for its own instructions only, not for those of inline asm.
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
 // What a block works on.
 struct Work { int b, h, tile, piece, pieces, slot; };
@@ -784,7 +781,7 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
         for (int r = 0; r < 4; ++r) {
           const f32x16& x = sc[n][r >> 1];
           const int v = (r & 1) * 8;
-          const float best = max3(max3(x[v], x[v + 1], x[v + 2]), max3(x[v + 3], x[v + 4], x[v + 5]), max3(x[v + 6], x[v + 7], x[v + 7])) * ks[r];
+          const float best = fmaxf(max3(max3(x[v], x[v + 1], x[v + 2]), x[v + 3], x[v + 4]), max3(x[v + 5], x[v + 6], x[v + 7])) * ks[r];
           tm = fmaxf(tm, best);
           tt = fmaxf(tt, best + lv[r]);
         }
