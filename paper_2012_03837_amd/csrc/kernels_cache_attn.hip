@@ -512,7 +512,7 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 ? 2 : 1) k_cache_attn(Cac
 }
 
 // ------------------------------------------------------------------------------------------------ many rows
-// The same for calls with many columns (prompts, chunks of them): a block has 128 columns or more, a wave 32 or 64 of them, and tiles of 64
+// The same for calls with many columns (prompts, chunks of them): a block has 128 columns, a wave 32 of them, and tiles of 64
 // tokens go through LDS, as numbers, for all its waves: keys in bf16, values in f16, each code converted once.  Products are 32 x 32 x 16; the rows of K are dealt
 // to tokens so that a lane's eight scores, and its operand of the second product, are eight tokens in order (token_of).
 // Weights enter the second product in f16, whose eleven bits leave 2^-12 of a weight (two parts in fp32, 2^-23): codes of 8 bits are f16 numbers too.  f16 has
@@ -579,18 +579,18 @@ __device__ __forceinline__ bool find_longest(const CacheView& c, const AttnArgs&
   return true;
 }
 
-// NB: head size in units of 32 columns, rounded up; CG: column groups of 32 of a wave.
+// NB: head size in units of 32 columns, rounded up.
 template <typename T, int NB>
 __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
   constexpr bool F = std::is_same<T, float>::value;
-  constexpr int CG = 1, QP = F ? 3 : 1, WP = F ? 2 : 1, DH = 32 * NB, KLD = DH + 8, VLD = 72, kLoads = (64 * (DH / 16) + 255) / 256;
+  constexpr int QP = F ? 3 : 1, WP = F ? 2 : 1, DH = 32 * NB, KLD = DH + 8, VLD = 72, kLoads = (64 * (DH / 16) + 255) / 256;
   constexpr float kTop = 7.f, kLag = 8.f;
   __shared__ __align__(16) bf16_t sk[2][64][KLD];
   __shared__ __align__(16) _Float16 sv[2][DH][VLD];
   __shared__ __align__(16) Runs runs[2];
   __shared__ __align__(8) unsigned short snan[2][DH][4];     // of a tile that not all columns see: which of a column's sixteen tokens are NaN
   const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-  const int dh = c.dh, page = 1 << c.shift, width = 128 * CG;
+  const int dh = c.dh, page = 1 << c.shift, width = 128;
   Work w;
   if (a.target) {
     if (!find_work(c, a, width, (unsigned)id, &w)) return;
@@ -601,7 +601,7 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
   const Sequence s = sequence_of(c, w.b);
   const int col0 = w.tile * width, columns = s.n * a.G;
   if (col0 >= columns) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 31, half = lane >> 5, first = col0 + wave * 32 * CG;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 31, half = lane >> 5, first = col0 + wave * 32;
 
   auto limit = [&](int t) {
     const int v = a.causal ? s.len - s.n + t + 1 : s.len;
@@ -609,7 +609,7 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
   };
   // visible tokens: of the block's first and last column there is, of the wave's, of the lane's
   const int blo = limit(col0 / a.G), bhi = limit((col0 + width < columns ? col0 + width - 1 : columns - 1) / a.G);
-  const int lo = limit(first / a.G), hi = first >= columns ? 0 : limit((first + 32 * CG < columns ? first + 32 * CG - 1 : columns - 1) / a.G);
+  const int lo = limit(first / a.G), hi = first >= columns ? 0 : limit((first + 32 < columns ? first + 31 : columns - 1) / a.G);
   int tile, last;
   tiles_of((((a.target ? s.len : bhi) + 63) >> 6), w.piece, w.pieces, &tile, &last);
   if (last > (bhi + 63) >> 6) last = (bhi + 63) >> 6;
@@ -632,12 +632,11 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
   };
   if (tile < last) look_up(tile);
 
-  int lim[CG];
-  bf16x8 qf[CG][2 * NB][QP];
-#pragma unroll
-  for (int n = 0; n < CG; ++n) {
-    const Column col = column_of(s, a, w.h, first + n * 32 + i);
-    lim[n] = col.there ? limit(col.t) : 0;
+  int lim;
+  bf16x8 qf[2 * NB][QP];
+  {
+    const Column col = column_of(s, a, w.h, first + i);
+    lim = col.there ? limit(col.t) : 0;
 #pragma unroll
     for (int k = 0; k < 2 * NB; ++k) {
       const int d = k * 16 + half * 8;
@@ -651,23 +650,17 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
           for (int e = 0; e < 8; ++e) v[e] = to_f(p[e]);
         }
       }
-      split8<QP>(v, qf[n][k]);
+      split8<QP>(v, qf[k]);
     }
   }
 
-  f32x16 acc[CG][NB];
-  float m[CG], top[CG], l[CG];           // largest score; largest score plus the logarithm of its values' scale; sum of weights
-  bool seen[CG];
+  f32x16 acc[NB];
+  float m = -INFINITY, top = -INFINITY, l = 0.f;      // largest score; largest score plus the logarithm of its values' scale; sum of weights
+  bool seen = false;
 #pragma unroll
-  for (int n = 0; n < CG; ++n) {
-    m[n] = top[n] = -INFINITY;
-    l[n] = 0.f;
-    seen[n] = false;
+  for (int j = 0; j < NB; ++j)
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[n][j][v] = 0.f;
-  }
+    for (int v = 0; v < 16; ++v) acc[j][v] = 0.f;
 
   // A tile on its way: sixteen bytes of a token's keys, and of a column's values, a thread and load.  No load is skipped: where there is no page, page 0 is read
   // and its scores and values are taken out; keys behind the head's columns are its last ones, against zeros of the query, and what comes of values there
@@ -747,7 +740,7 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
                   rv = *reinterpret_cast<const f32x4*>(&kn.rv[run0]);
       const int4 pg = *reinterpret_cast<const int4*>(&kn.here[run0]);
       const bool away = (pg.x & pg.y & pg.z & pg.w) == 0, masked = tok + 64 > lo || away;
-      f32x16 sc[CG][2];
+      f32x16 sc[2];
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         const bf16_t* kp = &sk[buf][g * 32 + token_of(i)][half * 8];
@@ -755,78 +748,73 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
         for (int k = 0; k < 2 * NB; ++k) {
           const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + k * 16);
 #pragma unroll
-          for (int n = 0; n < CG; ++n)
-#pragma unroll
-            for (int q = QP - 1; q >= 0; --q) sc[n][g] = mma32(kf, qf[n][k][q], k == 0 && q == QP - 1 ? f32x16{} : sc[n][g]);
+          for (int q = QP - 1; q >= 0; --q) sc[g] = mma32(kf, qf[k][q], k == 0 && q == QP - 1 ? f32x16{} : sc[g]);
         }
       }
-      f16x8 wf[CG][4][WP];
+      f16x8 wf[4][WP];
+      if (masked) {
+        const int here[4] = {pg.x, pg.y, pg.z, pg.w};
 #pragma unroll
-      for (int n = 0; n < CG; ++n) {
-        if (masked) {
-          const int here[4] = {pg.x, pg.y, pg.z, pg.w};
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const bool ok = here[r] && tok + r * 16 + half * 8 + e < lim[n];
-              sc[n][r >> 1][(r & 1) * 8 + e] = ok ? sc[n][r >> 1][(r & 1) * 8 + e] : -INFINITY;
-              seen[n] |= ok;
-            }
-        } else {
-          seen[n] = true;
-        }
-        float tm = -INFINITY, tt = -INFINITY;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const f32x16& x = sc[n][r >> 1];
-          const int v = (r & 1) * 8;
-          const float best = fmaxf(max3(max3(x[v], x[v + 1], x[v + 2]), x[v + 3], x[v + 4]), max3(x[v + 5], x[v + 6], x[v + 7])) * ks[r];
-          tm = fmaxf(tm, best);
-          tt = fmaxf(tt, best + lv[r]);
-        }
-        tm = both_max(tm);
-        tt = both_max(tt);
-        if (__ballot(tm > m[n] + kLag || tt > top[n] + kLag)) {
-          const float mn = fmaxf(m[n], tm), tn = fmaxf(top[n], tt);
-          l[n] *= mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - mn);
-          const float f = tn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top[n] - tn);
-#pragma unroll
-          for (int j = 0; j < NB; ++j) acc[n][j] *= f;
-          m[n] = mn;
-          top[n] = tn;
-        }
-        const float base = m[n] == -INFINITY ? 0.f : m[n], off = kTop - (top[n] == -INFINITY ? 0.f : top[n]);
-        // the exponent by which a weight with its values' scale is apart from the weight: where that, or the way back by the scale, leaves the range of
-        // 32 bits, the weights take an exponential of their own
-        const float apart = off + base, least = fminf(fminf(lv[0], lv[1]), fminf(lv[2], lv[3])) + apart;
-        const bool lost = __ballot(least < -100.f || fabsf(apart) > 100.f) != 0;
-        const float back = __builtin_amdgcn_exp2f(-apart);
-        if (lost) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) l[n] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][r >> 1][(r & 1) * 8 + e], ks[r], -base));
-        }
-        const float count = lost ? 0.f : back;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float up = lv[r] + off;
-          float p[8], sum = 0.f;
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][r >> 1][(r & 1) * 8 + e], ks[r], up));
-            sum += p[e];
+            const bool ok = here[r] && tok + r * 16 + half * 8 + e < lim;
+            sc[r >> 1][(r & 1) * 8 + e] = ok ? sc[r >> 1][(r & 1) * 8 + e] : -INFINITY;
+            seen |= ok;
           }
-          l[n] = __builtin_fmaf(sum, count * rv[r], l[n]);
+      } else {
+        seen = true;
+      }
+      float tm = -INFINITY, tt = -INFINITY;
 #pragma unroll
-          for (int q = 0; q < WP; ++q)
+      for (int r = 0; r < 4; ++r) {
+        const f32x16& x = sc[r >> 1];
+        const int v = (r & 1) * 8;
+        const float best = fmaxf(max3(max3(x[v], x[v + 1], x[v + 2]), x[v + 3], x[v + 4]), max3(x[v + 5], x[v + 6], x[v + 7])) * ks[r];
+        tm = fmaxf(tm, best);
+        tt = fmaxf(tt, best + lv[r]);
+      }
+      tm = both_max(tm);
+      tt = both_max(tt);
+      if (__ballot(tm > m + kLag || tt > top + kLag)) {
+        const float mn = fmaxf(m, tm), tn = fmaxf(top, tt);
+        l *= mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        const float f = tn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - tn);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              wf[n][r][q][e] = (_Float16)p[e];
-              if (q + 1 < WP) p[e] -= (float)wf[n][r][q][e];
-            }
+        for (int j = 0; j < NB; ++j) acc[j] *= f;
+        m = mn;
+        top = tn;
+      }
+      const float base = m == -INFINITY ? 0.f : m, off = kTop - (top == -INFINITY ? 0.f : top);
+      // the exponent by which a weight with its values' scale is apart from the weight: where that, or the way back by the scale, leaves the range of
+      // 32 bits, the weights take an exponential of their own
+      const float apart = off + base, least = fminf(fminf(lv[0], lv[1]), fminf(lv[2], lv[3])) + apart;
+      const bool lost = __ballot(least < -100.f || fabsf(apart) > 100.f) != 0;
+      const float back = __builtin_amdgcn_exp2f(-apart);
+      if (lost) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) l += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r >> 1][(r & 1) * 8 + e], ks[r], -base));
+      }
+      const float count = lost ? 0.f : back;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float up = lv[r] + off;
+        float p[8], sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r >> 1][(r & 1) * 8 + e], ks[r], up));
+          sum += p[e];
         }
+        l = __builtin_fmaf(sum, count * rv[r], l);
+#pragma unroll
+        for (int q = 0; q < WP; ++q)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            wf[r][q][e] = (_Float16)p[e];
+            if (q + 1 < WP) p[e] -= (float)wf[r][q][e];
+          }
       }
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
@@ -835,26 +823,21 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
         for (int r = 0; r < 4; ++r) {
           const f16x8 vf = *reinterpret_cast<const f16x8*>(vp + r * 16);
 #pragma unroll
-          for (int n = 0; n < CG; ++n)
-#pragma unroll
-            for (int q = WP - 1; q >= 0; --q) acc[n][j] = mma32(vf, wf[n][r][q], acc[n][j]);
+          for (int q = WP - 1; q >= 0; --q) acc[j] = mma32(vf, wf[r][q], acc[j]);
         }
       }
       if (tok + 64 > blo || away) {
         unsigned long long any = 0;
         for (int d = lane; d < DH; d += 64) any |= *reinterpret_cast<const unsigned long long*>(snan[buf][d]);
         if (__ballot(any != 0)) {
+          const int left = lim - tok;                     // bits of pages that are not there are zeros
+          const unsigned long long see = left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1;
 #pragma unroll
-          for (int n = 0; n < CG; ++n) {
-            const int left = lim[n] - tok;                     // bits of pages that are not there are zeros
-            const unsigned long long see = left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1;
+          for (int j = 0; j < NB; ++j)
 #pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-              for (int v = 0; v < 16; ++v)
-                if (*reinterpret_cast<const unsigned long long*>(snan[buf][j * 32 + 8 * (v / 4) + 4 * half + v % 4]) & see)
-                  acc[n][j][v] = __builtin_bit_cast(float, 0x7fc00000u);
-          }
+            for (int v = 0; v < 16; ++v)
+              if (*reinterpret_cast<const unsigned long long*>(snan[buf][j * 32 + 8 * (v / 4) + 4 * half + v % 4]) & see)
+                acc[j][v] = __builtin_bit_cast(float, 0x7fc00000u);
         }
       }
     }
@@ -862,43 +845,40 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
     __syncthreads();
   }
 
+  l += __shfl_xor(l, 32, 64);
+  int any = seen;
+  any |= __shfl_xor(any, 32, 64);
+  if (any && m == -INFINITY && l == 0.f) l = -1.f;
+  const int at = first + i;
+  const Column col = column_of(s, a, w.h, at);
+  // from the weights' reference to the scores', in two steps of half the exponent: one may leave the range
+  const float back = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(0.5f * (top - m - kTop));
 #pragma unroll
-  for (int n = 0; n < CG; ++n) {
-    l[n] += __shfl_xor(l[n], 32, 64);
-    int any = seen[n];
-    any |= __shfl_xor(any, 32, 64);
-    if (any && m[n] == -INFINITY && l[n] == 0.f) l[n] = -1.f;
-    const int at = first + n * 32 + i;
-    const Column col = column_of(s, a, w.h, at);
-    // from the weights' reference to the scores', in two steps of half the exponent: one may leave the range
-    const float back = top[n] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(0.5f * (top[n] - m[n] - kTop));
+  for (int j = 0; j < NB; ++j) acc[j] *= back;
+  if (!col.there) return;
+  if (w.pieces > 1) {
+    float* out = a.part + piece_at(c.B * c.Hkv * a.tiles, width, dh, w.slot);
+    if (half == 0) *reinterpret_cast<float2*>(out + width * dh + (at - col0) * 2) = make_float2(m, l);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) acc[n][j] *= back;
-    if (!col.there) continue;
-    if (w.pieces > 1) {
-      float* out = a.part + piece_at(c.B * c.Hkv * a.tiles, width, dh, w.slot);
-      if (half == 0) *reinterpret_cast<float2*>(out + width * dh + (at - col0) * 2) = make_float2(m[n], l[n]);
+    for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (int j = 0; j < NB; ++j)
+      for (int v = 0; v < 16; v += 4) {
+        const int d = j * 32 + 2 * v + 4 * half;
+        if (d < dh)
+          *reinterpret_cast<f32x4*>(out + (at - col0) * dh + d) = f32x4{acc[j][v] * back, acc[j][v + 1] * back, acc[j][v + 2] * back, acc[j][v + 3] * back};
+      }
+  } else {
+    const float f = over(m, l) * back;
+    T* out = (T*)a.o + col.row * a.ldo + col.head * dh;
+    if (a.lse && half == 0) a.lse[col.row * a.H + col.head] = log_sum(m, l);
 #pragma unroll
-        for (int v = 0; v < 16; v += 4) {
-          const int d = j * 32 + 2 * v + 4 * half;
-          if (d < dh)
-            *reinterpret_cast<f32x4*>(out + (at - col0) * dh + d) = f32x4{acc[n][j][v] * back, acc[n][j][v + 1] * back, acc[n][j][v + 2] * back, acc[n][j][v + 3] * back};
-        }
-    } else {
-      const float f = over(m[n], l[n]) * back;
-      T* out = (T*)a.o + col.row * a.ldo + col.head * dh;
-      if (a.lse && half == 0) a.lse[col.row * a.H + col.head] = log_sum(m[n], l[n]);
+    for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (int j = 0; j < NB; ++j)
-#pragma unroll
-        for (int v = 0; v < 16; v += 4) {
-          const int d = j * 32 + 2 * v + 4 * half;
-          if (d >= dh) continue;
-          put4(out + d, f32x4{acc[n][j][v] * f, acc[n][j][v + 1] * f, acc[n][j][v + 2] * f, acc[n][j][v + 3] * f}, a.vec);
-        }
-    }
+      for (int v = 0; v < 16; v += 4) {
+        const int d = j * 32 + 2 * v + 4 * half;
+        if (d >= dh) continue;
+        put4(out + d, f32x4{acc[j][v] * f, acc[j][v + 1] * f, acc[j][v + 2] * f, acc[j][v + 3] * f}, a.vec);
+      }
   }
 }
 
