@@ -515,10 +515,12 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 ? 2 : 1) k_cache_attn(Cac
 // The same for calls with many columns (prompts, chunks of them): a block has 128 columns, a wave 32 of them, and tiles of 64
 // tokens go through LDS, as numbers, for all its waves: keys in bf16, values in f16, each code converted once.  Products are 32 x 32 x 16; the rows of K are dealt
 // to tokens so that a lane's eight scores, and its operand of the second product, are eight tokens in order (token_of).
-// Weights enter the second product in f16, whose eleven bits leave 2^-12 of a weight (two parts in fp32, 2^-23): codes of 8 bits are f16 numbers too.  f16 has
-// no range to speak of, so that they are held relative to the largest weight times scale of the values that the row has met (`top`), at 2^7 of which one stands;
-// both it and the largest score lag by a factor of up to 2^8, so that sums are seldom rescaled.  Weights down to 2^-21 of the largest have all their bits, 2^-32 of it is
-// lost of others.  One exponential gives a weight with its values' scale; the sum of weights takes the scale out again, run by run, and is of 32-bit numbers.
+// In fp32 weights enter the second product in three bf16 parts, all their 24 bits; in bf16 in f16, whose eleven bits leave 2^-12 of a weight: codes of 8 bits are f16 numbers too.  Neither
+// has room for a weight times any scale of its values, so that they are held relative to the largest such product that the row has met (`top`), at 2^7 of which one stands; both it
+// and the largest score lag by a factor of up to 2^8, so that sums are seldom rescaled.  One exponential gives a weight with its values' scale; the sum of weights takes the scale out
+// again, run by run, and is of 32-bit numbers.  In f16 2^-32 of `top` is lost of small products, which a page of a larger scale may be the cause of while its numbers in a column are zeros: where `top` is
+// more than 2^8 times the row's largest weight times the scale of a run of the tile, the tile's weights are two bf16 parts (2^-16 of a weight; bf16 has the range of fp32).  So of a value
+// 2^-24 of the row's largest weight is lost at most, whatever the other pages hold.
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 
@@ -530,6 +532,18 @@ __device__ __forceinline__ f16x8 codes8_f16(unsigned a, unsigned b) {
   f16x8 v;
   v[0] = p[0]; v[1] = p[1]; v[2] = q[0]; v[3] = q[1]; v[4] = r[0]; v[5] = r[1]; v[6] = s[0]; v[7] = s[1];
   return v;
+}
+template <typename V> __device__ __forceinline__ auto codes8_as(unsigned a, unsigned b) {
+  if constexpr (std::is_same<V, bf16_t>::value) return codes8(a, b);
+  else return codes8_f16(a, b);
+}
+// Codes that stand in f16, in bf16: both hold them.
+__device__ __forceinline__ bf16x8 in_bf16(const bf16x8& v) { return v; }
+__device__ __forceinline__ bf16x8 in_bf16(const f16x8& v) {
+  bf16x8 r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = (bf16_t)(float)v[e];
+  return r;
 }
 // Token of a tile of 32 that row `r` of a product stands for: values 8 kk .. 8 kk + 7 of lane l are rows 16 kk + 4 (l / 32) + {0..3, 8..11}, tokens
 // 16 kk + 8 (l / 32) + {0..7}.
@@ -583,10 +597,12 @@ __device__ __forceinline__ bool find_longest(const CacheView& c, const AttnArgs&
 template <typename T, int NB>
 __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView c, AttnArgs a) {
   constexpr bool F = std::is_same<T, float>::value;
-  constexpr int QP = F ? 3 : 1, WP = F ? 2 : 1, DH = 32 * NB, KLD = DH + 8, VLD = 72, kLoads = (64 * (DH / 16) + 255) / 256;
-  constexpr float kTop = 7.f, kLag = 8.f;
+  constexpr int QP = F ? 3 : 1, WP = F ? 3 : 2, DH = 32 * NB, KLD = DH + 8, VLD = 72, kLoads = (64 * (DH / 16) + 255) / 256;
+  constexpr float kTop = 7.f, kLag = 8.f, kLeast = F ? -60.f : kTop - 8.f;
+  typedef typename std::conditional<F, bf16_t, _Float16>::type V;            // numbers that values are held in
+  typedef __attribute__((ext_vector_type(8))) V V8;
   __shared__ __align__(16) bf16_t sk[2][64][KLD];
-  __shared__ __align__(16) _Float16 sv[2][DH][VLD];
+  __shared__ __align__(16) V sv[2][DH][VLD];
   __shared__ __align__(16) Runs runs[2];
   __shared__ __align__(8) unsigned short snan[2][DH][4];     // of a tile that not all columns see: which of a column's sixteen tokens are NaN
   const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
@@ -712,8 +728,8 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
           }
           snan[buf][e][run] = (unsigned short)bits;
         }
-        *reinterpret_cast<f16x8*>(&sv[buf][e][run * 16]) = codes8_f16(q[0], q[1]);
-        *reinterpret_cast<f16x8*>(&sv[buf][e][run * 16 + 8]) = codes8_f16(q[2], q[3]);
+        *reinterpret_cast<V8*>(&sv[buf][e][run * 16]) = codes8_as<V>(q[0], q[1]);
+        *reinterpret_cast<V8*>(&sv[buf][e][run * 16 + 8]) = codes8_as<V>(q[2], q[3]);
       }
     }
   };
@@ -751,7 +767,6 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
           for (int q = QP - 1; q >= 0; --q) sc[g] = mma32(kf, qf[k][q], k == 0 && q == QP - 1 ? f32x16{} : sc[g]);
         }
       }
-      f16x8 wf[4][WP];
       if (masked) {
         const int here[4] = {pg.x, pg.y, pg.z, pg.w};
 #pragma unroll
@@ -786,45 +801,57 @@ __global__ void __launch_bounds__(256, NB <= 4 ? 2 : 1) k_cache_prompt(CacheView
         top = tn;
       }
       const float base = m == -INFINITY ? 0.f : m, off = kTop - (top == -INFINITY ? 0.f : top);
-      // the exponent by which a weight with its values' scale is apart from the weight: where that, or the way back by the scale, leaves the range of
-      // 32 bits, the weights take an exponential of their own
+      // a weight with its values' scale stands at 2^(apart + lv) of the weight: where that is too little, or the way back leaves the range of 32 bits, it is taken from the weight
       const float apart = off + base, least = fminf(fminf(lv[0], lv[1]), fminf(lv[2], lv[3])) + apart;
-      const bool lost = __ballot(least < -100.f || fabsf(apart) > 100.f) != 0;
-      const float back = __builtin_amdgcn_exp2f(-apart);
-      if (lost) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) l += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r >> 1][(r & 1) * 8 + e], ks[r], -base));
-      }
-      const float count = lost ? 0.f : back;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float up = lv[r] + off;
-        float p[8], sum = 0.f;
+      const bool thin = __ballot(least < kLeast || fabsf(apart) > 100.f) != 0;
+      const float back = thin ? 0.f : __builtin_amdgcn_exp2f(-apart);
+      auto weights = [&](int r, float up, float count, float (&p)[8]) {
+        float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r >> 1][(r & 1) * 8 + e], ks[r], up));
           sum += p[e];
         }
-        l = __builtin_fmaf(sum, count * rv[r], l);
-#pragma unroll
-        for (int q = 0; q < WP; ++q)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            wf[r][q][e] = (_Float16)p[e];
-            if (q + 1 < WP) p[e] -= (float)wf[r][q][e];
-          }
-      }
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        const _Float16* vp = &sv[buf][j * 32 + i][half * 8];
+        l = __builtin_fmaf(sum, count, l);
+      };
+      auto values = [&](int j, int r) { return *reinterpret_cast<const V8*>(&sv[buf][j * 32 + i][half * 8 + r * 16]); };
+      if (F || thin) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const f16x8 vf = *reinterpret_cast<const f16x8*>(vp + r * 16);
+          float p[8];
+          bf16x8 wf[WP];
+          if (thin) {
+            const float e = fmaxf(lv[r] + apart, kTop), f = __builtin_amdgcn_exp2f(fminf(lv[r] + apart - kTop, 0.f));
+            weights(r, e - base, __builtin_amdgcn_exp2f(-e), p);
 #pragma unroll
-          for (int q = WP - 1; q >= 0; --q) acc[j] = mma32(vf, wf[r][q], acc[j]);
+            for (int q = 0; q < 8; ++q) p[q] *= f;
+          } else {
+            weights(r, lv[r] + off, back * rv[r], p);
+          }
+          split8<WP>(p, wf);
+#pragma unroll
+          for (int j = 0; j < NB; ++j) {
+            const bf16x8 vf = in_bf16(values(j, r));
+#pragma unroll
+            for (int q = WP - 1; q >= 0; --q) acc[j] = mma32(vf, wf[q], acc[j]);
+            if (!F) __builtin_amdgcn_sched_barrier(0);     // seldom taken: no registers beyond those of the other way
+          }
         }
+      }
+      if constexpr (!F) {
+        const float in = thin ? -INFINITY : off;           // all weights are zeros then: a way around would cost the sums their place in registers
+        f16x8 wf[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float p[8];
+          weights(r, lv[r] + in, back * rv[r], p);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) wf[r][e] = (_Float16)p[e];
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[j] = mma32(values(j, r), wf[r], acc[j]);
       }
       if (tok + 64 > blo || away) {
         unsigned long long any = 0;

@@ -1,9 +1,11 @@
-"""Attention over the 8-bit cache where its kernels take ways of their own.  Tolerances are those of test_gpu_cache."""
+"""Attention over the 8-bit cache where its kernels take ways of their own.  Tolerances are those of test_gpu_cache but where they are
+named."""
 import numpy as np
 import pytest
 
 from oracle import cache as C
 from test_gpu_cache import K, Cache, attend, right  # noqa: F401
+from test_gpu_residual import HALF, host
 
 pytestmark = pytest.mark.gpu
 
@@ -27,3 +29,47 @@ def test_largest_scores_of_the_last_columns(K, dtype, T, page, dh):  # noqa: F81
     o, lse, q, _ = attend(K, c, 1, causal=0, q=q)
     right(c, 1, 0, o, lse, q)
 
+
+
+# ------------------------------------------------------------------------------------------------ small weights, small values
+def near_of_their_own(c, o, q):
+    """Every column by what stands in it.  One rounding of the output; a weight as in test_gpu_cache (in 24 bits in fp32, 2^-16 in bf16, 2^-12 with many rows) and in bf16 with many
+    rows, whose weights end at 2^-32 of a reference that is 2^8 times the row's largest at most, 2^-24 of that for each token: of its |v|, whatever stands in other columns."""
+    ref, _, size, mass = C.attention(q.astype(np.float64).reshape(c.rows, c.Hkv, c.dh), c.kp, c.vp, c.ks, c.vs, c.seqs(), c.table, False)
+    n, many, new = int(c.lens[0]), c.T > 32, int(c.starts[1])
+    v = np.abs(c.vp * c.vs[..., None, None])[c.table[0]]                     # [pages, heads, dh, page]
+    total = v.sum((0, 3)) if many and c.dtype else 0.0
+    rel = 2 * (2 * 2.0 ** -24 * (c.dh + 8) * size + 2.0 ** -22) + {(1, True): 2.0 ** -12, (1, False): 2.0 ** -16}.get((c.dtype, many), 2.0 ** -24) + 2 * 2.0 ** -24 * (n / 16 + 64)
+    err = np.abs(host(o)[:new].reshape(ref[:new].shape) - ref[:new])
+    assert (err <= 1.01 * HALF[c.dtype] * np.abs(ref[:new]) + rel[:new, :, None] * mass[:new] + 2.0 ** -24 * total).all()
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("T", [1, 20, 130])
+@pytest.mark.parametrize("up", [6, 9, 14, 20, 30, 60, 100])
+@pytest.mark.parametrize("page,dh", [(64, 64), (32, 128), (16, 192)])
+def test_values_beside_pages_of_large_scales(K, dtype, T, up, page, dh):  # noqa: F811
+    """Every third page has large values in one column, zeros in the others: those are the other pages' values all the same."""
+    c = Cache(dtype, 19, [T], [512], 1, dh, page)
+    large = c.table[0][1::3]
+    c.vp[large, :, 1:], c.vs[large] = 0.0, 2.0 ** up
+    c.load()
+    o, _, q, _ = attend(K, c, 1, causal=0)
+    near_of_their_own(c, o, q)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("T", [1, 20, 130])
+@pytest.mark.parametrize("down", [4, 9, 14])
+def test_small_weights_beside_a_large_one(K, dtype, T, down):  # noqa: F811
+    """One token has 2^down times the weight of the others and values in one column only."""
+    c = Cache(dtype, 23, [T], [2048], 1, 64, 64)
+    p, at = c.table[0, 700 // 64], 700 % 64
+    c.kp[..., 63], c.ks[:], c.kp[p, 0, at] = 0.0, 2.0 ** -5, 0.0
+    c.kp[p, 0, at, 63] = C.e4m3(down * np.log(2) * 8 * 2.0 ** 5 / 8)
+    c.vp[p, 0, 1:, at] = 0.0
+    c.load()
+    q = c.rnd(c.rows, 64)
+    q[:, 63] = 8.0
+    o, _, q, _ = attend(K, c, 1, causal=0, q=q)
+    near_of_their_own(c, o, q)
