@@ -266,12 +266,19 @@ def lpk_rotary(dtype, x, y, pos, freq, rows, S, heads, dh, rot, interleaved=0, s
 
 
 def _pages(table, kpages, B, Hkv, dh, page):
-    """Page numbers of a sequence in the table, and pages in the pools."""
-    return (0 if table is None else table.numel() // max(1, B)), (0 if kpages is None else kpages.numel() // max(1, Hkv * dh * page))
+    """Page numbers of a sequence in the table (in one dimension: of B sequences, one behind another), and pages in the pools."""
+    n = 0 if kpages is None else kpages.numel() // max(1, Hkv * dh * page)
+    if table is None:
+        return 0, n
+    if table.dim() == 2:
+        return table.shape[1], n
+    if table.dim() == 1:
+        return table.numel() // max(1, B), n
+    raise KernelError(f"table of {tuple(table.shape)}: a row of page numbers for each of {B} sequences is needed")
 
 
 def lpk_cache_append(dtype, k, v, starts, lens, table, kpages, vpages, kscale, vscale, B, T, Hkv, dh, page):
-    """k and v: matrices, their rows any distance apart.  The table has B rows, the pools as many pages as kpages holds."""
+    """k and v: matrices, their rows any distance apart.  The table has a row for each sequence, B or more, as long as it has columns; the pools as many pages as kpages holds."""
     e, dev = _T.get(dtype) or _real(dtype), _none("lpk_cache_append") if k is None else k.get_device()
     (most, n), i32, f, q, rows = _pages(table, kpages, B, Hkv, dh, page), _T["i32"], _T[0], _T["e4m3"], k.shape[0]
     _run("lpk_cache_append", dev, dtype, *_mat(k, e, rows, Hkv * dh, dev), *_mat(v, e, rows, Hkv * dh, dev), rows, _at(starts, i32, B + 1, dev),

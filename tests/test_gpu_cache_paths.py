@@ -73,3 +73,22 @@ def test_small_weights_beside_a_large_one(K, dtype, T, down):  # noqa: F811
     q[:, 63] = 8.0
     o, _, q, _ = attend(K, c, 1, causal=0, q=q)
     near_of_their_own(c, o, q)
+
+
+# ------------------------------------------------------------------------------------------------ tables of all slots
+def test_a_table_with_more_rows_than_sequences(K):  # noqa: F811
+    """The first rows of a program's table of slots: its other rows, which name the same pages, are not read."""
+    import torch
+    c = Cache(1, 29, [1, 40], [70, 200], 2, 64, 32)
+    o, lse, q, _ = attend(K, c, 2)
+    (k, kn), (v, vn) = c.matrix(128), c.matrix(128)
+    c.dtable = torch.cat([c.dtable, c.dtable.flip(0), c.dtable.flip(1)])
+    o2, lse2, _, _ = attend(K, c, 2, q=q)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    K.lpk_cache_append(1, k, v, *c.paged(), *c.size())
+    for x, pool, scale, dpool, values in ((kn, c.kp, c.ks, c.dkp, False), (vn, c.vp, c.vs, c.dvp, True)):
+        C.append(x.reshape(c.rows, 2, 64), pool, scale, values, c.seqs(), c.table)
+        assert np.array_equal(host(dpool), pool)
+    a, b = torch.zeros_like(k).contiguous(), torch.zeros_like(v).contiguous()
+    K.lpk_cache_read(1, a, b, *c.paged(), *c.size())
+    assert np.array_equal(host(a), C.read(c.kp, c.ks, False, c.seqs(), c.table, c.rows).reshape(c.rows, -1))
