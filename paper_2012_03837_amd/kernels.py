@@ -249,20 +249,25 @@ def _mat(t, types, rows, cols, dev):
 def lpk_rotary_frequencies(rot, base=10000.0, factor=1.0, low=1.0, high=1.0, context=0.0):
     """Host tensor of rot / 2 doubles, radians a position; needs no device."""
     import torch
-    freq = torch.empty(max(0, rot) // 2, dtype=torch.float64)
+    if rot >> 31:
+        _wide(rot)
+    freq = torch.empty(rot // 2, dtype=torch.float64)
     _ck(_fn("lpk_rotary_frequencies")(freq.data_ptr(), rot, base, factor, low, high, context), "lpk_rotary_frequencies")
     return freq
 
 
-def _wide(n):
-    raise KernelError(f"{n}: a number of 31 bits is needed")
+def _wide(*n):
+    """For numbers that would reach a call cut to 32 bits, when the tensors have been compared with what they were before."""
+    raise KernelError(f"{', '.join(map(str, n))}: numbers of 31 bits are needed")
 
 
 def lpk_rotary(dtype, x, y, pos, freq, rows, S, heads, dh, rot, interleaved=0, scale=1.0, backward=0):
     """x and y: matrices, their rows any distance apart (the q and k columns of qkv, say)."""
     e, dev = _T.get(dtype) or _real(dtype), _none("lpk_rotary") if x is None else x.get_device()
+    if (rows | S | heads | dh | rot) >> 31:
+        _wide(rows, S, heads, dh, rot)
     _run("lpk_rotary", dev, dtype, *_mat(x, e, rows, heads * dh, dev), *_mat(y, e, rows, heads * dh, dev), _at(pos, _T["i32"], rows, dev),
-         _at(freq, _T["f64"], rot // 2, dev), rows, S if -1 < S < 1 << 31 else _wide(S), heads, dh, rot, 1 if interleaved else 0, scale, 1 if backward else 0)
+         _at(freq, _T["f64"], rot // 2, dev), rows, S, heads, dh, rot, 1 if interleaved else 0, scale, 1 if backward else 0)
 
 
 def _pages(table, kpages, B, Hkv, dh, page):
@@ -281,31 +286,37 @@ def lpk_cache_append(dtype, k, v, starts, lens, table, kpages, vpages, kscale, v
     """k and v: matrices, their rows any distance apart.  The table has a row for each sequence, B or more, as long as it has columns; the pools as many pages as kpages holds."""
     e, dev = _T.get(dtype) or _real(dtype), _none("lpk_cache_append") if k is None else k.get_device()
     (most, n), i32, f, q, rows = _pages(table, kpages, B, Hkv, dh, page), _T["i32"], _T[0], _T["e4m3"], k.shape[0]
+    if (B | T | Hkv | dh | page | rows | most | n) >> 31:
+        _wide(B, T, Hkv, dh, page, rows, most, n)
     _run("lpk_cache_append", dev, dtype, *_mat(k, e, rows, Hkv * dh, dev), *_mat(v, e, rows, Hkv * dh, dev), rows, _at(starts, i32, B + 1, dev),
          _at(lens, i32, B, dev), _at(table, i32, B * most, dev), _at(kpages, q, 0, dev), _at(vpages, q, n * Hkv * dh * page, dev), _at(kscale, f, n * Hkv, dev),
-         _at(vscale, f, n * Hkv, dev), B, T if -1 < T < 1 << 31 else _wide(T), Hkv, dh, page, most, n)
+         _at(vscale, f, n * Hkv, dev), B, T, Hkv, dh, page, most, n)
 
 
 def lpk_cache_read(dtype, k, v, starts, lens, table, kpages, vpages, kscale, vscale, B, T, Hkv, dh, page):
     e, dev = _T.get(dtype) or _real(dtype), _none("lpk_cache_read") if k is None else k.get_device()
     (most, n), i32, f, q, rows = _pages(table, kpages, B, Hkv, dh, page), _T["i32"], _T[0], _T["e4m3"], k.shape[0]
+    if (B | T | Hkv | dh | page | rows | most | n) >> 31:
+        _wide(B, T, Hkv, dh, page, rows, most, n)
     _run("lpk_cache_read", dev, dtype, *_mat(k, e, rows, Hkv * dh, dev), *_mat(v, e, rows, Hkv * dh, dev), rows, _at(starts, i32, B + 1, dev),
          _at(lens, i32, B, dev), _at(table, i32, B * most, dev), _at(kpages, q, 0, dev), _at(vpages, q, n * Hkv * dh * page, dev), _at(kscale, f, n * Hkv, dev),
-         _at(vscale, f, n * Hkv, dev), B, T if -1 < T < 1 << 31 else _wide(T), Hkv, dh, page, most, n)
+         _at(vscale, f, n * Hkv, dev), B, T, Hkv, dh, page, most, n)
 
 
 def lpk_cache_attention_scratch(B, T, H, Hkv, dh, page, max_pages):
-    """Floats of workspace; needs no device."""
-    return _fn("lpk_cache_attention_scratch")(B, T, H, Hkv, dh, page, max_pages)
+    """Floats of workspace (0 for what the call refuses); needs no device."""
+    return 0 if (B | T | H | Hkv | dh | page | max_pages) >> 31 else _fn("lpk_cache_attention_scratch")(B, T, H, Hkv, dh, page, max_pages)
 
 
 def lpk_cache_attention(dtype, q, starts, lens, table, kpages, vpages, kscale, vscale, o, lse, B, T, H, Hkv, dh, page, causal=1, scratch=None):
     """q and o: matrices, their rows any distance apart."""
     e, dev = _T.get(dtype) or _real(dtype), _none("lpk_cache_attention") if q is None else q.get_device()
     (most, n), i32, f, e8, rows = _pages(table, kpages, B, Hkv, dh, page), _T["i32"], _T[0], _T["e4m3"], q.shape[0]
+    if (B | T | H | Hkv | dh | page | rows | most | n) >> 31:
+        _wide(B, T, H, Hkv, dh, page, rows, most, n)
     _run("lpk_cache_attention", dev, dtype, *_mat(q, e, rows, H * dh, dev), rows, _at(starts, i32, B + 1, dev), _at(lens, i32, B, dev),
          _at(table, i32, B * most, dev), _at(kpages, e8, 0, dev), _at(vpages, e8, n * Hkv * dh * page, dev), _at(kscale, f, n * Hkv, dev),
-         _at(vscale, f, n * Hkv, dev), *_mat(o, e, rows, H * dh, dev), _at(lse, f, rows * H, dev), B, T if -1 < T < 1 << 31 else _wide(T), H, Hkv, dh, page, most, n, 1 if causal else 0,
+         _at(vscale, f, n * Hkv, dev), *_mat(o, e, rows, H * dh, dev), _at(lse, f, rows * H, dev), B, T, H, Hkv, dh, page, most, n, 1 if causal else 0,
          _at(scratch, f, 0, dev), _size(scratch))
 
 
