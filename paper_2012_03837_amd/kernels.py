@@ -167,17 +167,24 @@ def _run(name, dev, *args):
         _ck(rc, name)
 
 
+def _wide(*n):
+    """For numbers that would reach a call cut to 32 bits, when the tensors have been compared with what they were before."""
+    raise KernelError(f"{', '.join(map(str, n))}: numbers of 31 bits are needed")
+
+
 def _size(t):
     return 0 if t is None else t.numel()
 
 
 def lpk_linear_attention_scratch(B, S, H, dh, backward):
-    """Floats of workspace; needs no device."""
-    return _fn("lpk_linear_attention_scratch")(B, S, H, dh, backward)
+    """Floats of workspace (0 for what the calls refuse); needs no device."""
+    return 0 if (B | S | H | dh) >> 31 else _fn("lpk_linear_attention_scratch")(B, S, H, dh, backward)
 
 
 def lpk_linear_attention_fwd(dtype, qkv, log_decay, lens, s0, o, s_out, B, S, H, dh, scratch=None):
     e, dev = _T.get(dtype) or _real(dtype), _none("lpk_linear_attention_fwd") if qkv is None else qkv.get_device()
+    if (B | S | H | dh) < 0:
+        _wide(B, S, H, dh)
     e = e if S else None
     f, n, state = _T[0], B * S * H * dh, B * H * dh * dh
     _run("lpk_linear_attention_fwd", dev, dtype, _at(qkv, e, 3 * n, dev), _at(log_decay, f, H, dev), _at(lens, _T["i32"], B, dev),
@@ -186,6 +193,8 @@ def lpk_linear_attention_fwd(dtype, qkv, log_decay, lens, s0, o, s_out, B, S, H,
 
 def lpk_linear_attention_bwd(dtype, qkv, log_decay, lens, s0, dout, ds_out, dqkv, ds0, B, S, H, dh, scratch=None):
     e, dev = _T.get(dtype) or _real(dtype), _none("lpk_linear_attention_bwd") if qkv is None else qkv.get_device()
+    if (B | S | H | dh) < 0:
+        _wide(B, S, H, dh)
     e = e if S else None
     f, n, state = _T[0], B * S * H * dh, B * H * dh * dh
     _run("lpk_linear_attention_bwd", dev, dtype, _at(qkv, e, 3 * n, dev), _at(log_decay, f, H, dev), _at(lens, _T["i32"], B, dev),
@@ -195,6 +204,8 @@ def lpk_linear_attention_bwd(dtype, qkv, log_decay, lens, s0, dout, ds_out, dqkv
 
 def lpk_linear_attention_step(dtype, qkv, log_decay, state, o, B, H, dh):
     e, dev, n = _T.get(dtype) or _real(dtype), _none("lpk_linear_attention_step") if qkv is None else qkv.get_device(), B * H * dh
+    if (B | H | dh) < 0:
+        _wide(B, H, dh)
     f = _T[0]
     _run("lpk_linear_attention_step", dev, dtype, _at(qkv, e, 3 * n, dev), _at(log_decay, f, H, dev), _at(state, f, n * dh, dev), _at(o, e, n, dev),
          B, H, dh)
@@ -213,12 +224,14 @@ def lpk_dropout(dtype, x, res, y, p, rng, site):
 
 
 def lpk_rmsnorm_scratch(rows, d):
-    """Floats of workspace; needs no device."""
-    return _fn("lpk_rmsnorm_scratch")(rows, d)
+    """Floats of workspace (0 for what the call refuses); needs no device."""
+    return 0 if (rows | d) >> 31 else _fn("lpk_rmsnorm_scratch")(rows, d)
 
 
 def lpk_rmsnorm_fwd(dtype, x, res, g, r, y, y8, y8_scale, rstd, rows, d, eps, p=0.0, rng=None, site=0):
     e, dev, n = _T.get(dtype) or _real(dtype), _none("lpk_rmsnorm_fwd") if x is None else x.get_device(), rows * d
+    if (rows | d) < 0:
+        _wide(rows, d)
     f = _T[0]
     _run("lpk_rmsnorm_fwd", dev, dtype, _at(x, e, n, dev), _at(res, e, n, dev), _at(g, f, d, dev), _at(r, e, n, dev), _at(y, e, n, dev),
          _at(y8, _T["e4m3"], n, dev), _at(y8_scale, f, rows, dev), _at(rstd, f, rows, dev), rows, d, eps, p, _at(rng, _T["u64"], 2, dev),
@@ -227,6 +240,8 @@ def lpk_rmsnorm_fwd(dtype, x, res, g, r, y, y8, y8_scale, rstd, rows, d, eps, p=
 
 def lpk_rmsnorm_bwd(dtype, dy, r, rstd, g, add, dres, dx, dg, rows, d, accumulate=0, scratch=None, p=0.0, rng=None, site=0):
     e, dev, n = _T.get(dtype) or _real(dtype), _none("lpk_rmsnorm_bwd") if dy is None else dy.get_device(), rows * d
+    if (rows | d) < 0:
+        _wide(rows, d)
     f = _T[0]
     _run("lpk_rmsnorm_bwd", dev, dtype, _at(dy, e, n, dev), _at(r, e, n, dev), _at(rstd, f, rows, dev), _at(g, f, d, dev), _at(add, e, n, dev),
          _at(dres, e, n, dev), _at(dx, e, n, dev), _at(dg, f, d, dev), rows, d, accumulate, p, _at(rng, _T["u64"], 2, dev),
@@ -254,11 +269,6 @@ def lpk_rotary_frequencies(rot, base=10000.0, factor=1.0, low=1.0, high=1.0, con
     freq = torch.empty(rot // 2, dtype=torch.float64)
     _ck(_fn("lpk_rotary_frequencies")(freq.data_ptr(), rot, base, factor, low, high, context), "lpk_rotary_frequencies")
     return freq
-
-
-def _wide(*n):
-    """For numbers that would reach a call cut to 32 bits, when the tensors have been compared with what they were before."""
-    raise KernelError(f"{', '.join(map(str, n))}: numbers of 31 bits are needed")
 
 
 def lpk_rotary(dtype, x, y, pos, freq, rows, S, heads, dh, rot, interleaved=0, scale=1.0, backward=0):
