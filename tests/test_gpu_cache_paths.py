@@ -92,3 +92,64 @@ def test_a_table_with_more_rows_than_sequences(K):  # noqa: F811
     a, b = torch.zeros_like(k).contiguous(), torch.zeros_like(v).contiguous()
     K.lpk_cache_read(1, a, b, *c.paged(), *c.size())
     assert np.array_equal(host(a), C.read(c.kp, c.ks, False, c.seqs(), c.table, c.rows).reshape(c.rows, -1))
+
+
+# ------------------------------------------------------------------------------------------------ blocks and their work
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("causal", [1, 0])
+@pytest.mark.parametrize("page,length", [(16, 4217), (64, 4217), (256, 2100), (32, 2049)])
+def test_long_axes_that_stay_whole(K, dtype, causal, page, length):  # noqa: F811
+    """Enough heads and sequences that no axis is divided, and more than 32 and 64 tiles of 64 tokens a block, whose pages are looked up 32 tiles at a time; some are
+    missing around those borders."""
+    B, heads, used = 8, 64, -(-length // page)
+    c = Cache(dtype, page, [35] + [1] * (B - 1), [60] * B, heads, 16, page, most=-(-used // B) + 1)
+    c.table = np.full((B, used), -1, np.int32)
+    order = c.rng.permutation(c.pages)
+    c.table[0], c.table[1:, 0] = order[:used], order[used:used + B - 1]
+    for tile in (32, 64):
+        at = tile * 64 // page
+        c.table[0, at - 1:at], c.table[0, at + 1:at + 2] = -1, -1
+    c.lens = np.array([length] + [9] * (B - 1), np.int32)
+    c.load()
+    assert K.lpk_cache_attention_scratch(B, c.T, heads, heads, 16, page, used) == 0                  # nothing is divided
+    o, lse, q, _ = attend(K, c, 1, causal)
+    right(c, 1, causal, o, lse, q)
+    assert c.guards_stand()
+
+
+def ragged(rng, B, T, most):
+    """New rows and lengths of B sequences: none, one, T and what lies between; some without rows, some without tokens."""
+    new = np.minimum(rng.integers(0, T + 1, B), rng.integers(0, T + 1, B))
+    new[rng.integers(0, B, B // 5)], new[rng.integers(0, B, B // 8)] = 1, 0
+    new[B // 2] = T
+    lens = np.maximum(rng.integers(0, most + 1, B), new)
+    lens[rng.integers(0, B, 3)] = most
+    lens[(new < 2) & (rng.random(B) < 0.1)] = 0
+    return [int(n) for n in new], [int(n) for n in lens]
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("B,T,most,Hkv,G,dh,page,divided", [
+    (65, 1, 2500, 1, 2, 16, 16, True), (130, 1, 700, 2, 1, 32, 64, True), (130, 4, 700, 2, 3, 16, 32, True), (200, 1, 300, 1, 4, 64, 64, False),
+    (70, 150, 500, 1, 1, 16, 16, False), (130, 45, 700, 4, 1, 16, 64, False), (70, 140, 900, 2, 1, 32, 32, True), (129, 20, 650, 1, 3, 16, 16, True)])
+def test_many_sequences(K, dtype, B, T, most, Hkv, G, dh, page, divided):  # noqa: F811
+    """More sequences than a wave has lanes, ragged, few rows and many, axes whole and divided."""
+    new, lens = ragged(np.random.default_rng(B + T), B, T, most)
+    c = Cache(dtype, B, new, lens, Hkv, dh, page)
+    assert (K.lpk_cache_attention_scratch(B, c.T, Hkv * G, Hkv, dh, page, c.table.shape[1]) > 0) == divided
+    o, lse, q, _ = attend(K, c, G)
+    right(c, G, 1, o, lse, q)
+    assert c.guards_stand()
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("B,chunk,most", [(12, 300, 900), (64, 200, 400), (90, 130, 700)])
+def test_single_tokens_beside_a_chunk(K, dtype, B, chunk, most):  # noqa: F811
+    """A server's step: one user's chunk of a prompt among others' single tokens."""
+    rng = np.random.default_rng(B)
+    new, lens = [1] * B, [int(n) for n in rng.integers(1, most + 1, B)]
+    new[B // 3], lens[B // 3] = chunk, most
+    c = Cache(dtype, B + 1, new, lens, 1, 64, 64)
+    o, lse, q, _ = attend(K, c, 2)
+    right(c, 2, 1, o, lse, q)
+    assert c.guards_stand()
