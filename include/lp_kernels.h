@@ -143,7 +143,8 @@ size_t lpk_rmsnorm_scratch(int rows, int d);
  *   y = scale (a cos t - b sin t, a sin t + b cos t);      backward: the transpose, the gradient of x from that of y.
  * x and y: `rows` rows of heads * dh columns (dh up to 512) with leading dimensions ldx and ldy; columns rot .. dh - 1 of a head (rot even) are copied;
  * y may be x (ldy = ldx), otherwise they do not overlap.  pos int32 [rows] on the device, any number (null: row % S); freq fp64 [rot/2] on
- * the device, radians a position: the product is taken in 64 bits.  rows up to 2^30, heads * dh up to 2^24, leading dimensions to 2^32.
+ * the device, radians a position: the product is taken in 64 bits, its whole turns are taken off, and sine and cosine are those of the rest as a 32-bit number of half turns.
+ * rows up to 2^30, heads * dh up to 2^24, leading dimensions to 2^32.
  * lpk_rotary_frequencies writes such a table to host memory: base^(-2 i / rot), stretched for contexts longer than those trained on: divided by
  * `factor` where a pair turns at most `low` times within `context` positions, kept where it turns `high` times or more, in between blended in the number of
  * turns (factor 1: kept; low = high = infinity: all divided). */
@@ -170,7 +171,10 @@ int lpk_rotary_frequencies(double* freq, int rot, double base, double factor, do
  * Attention: o = softmax(q k^T dh^-1/2) v for the rows of q [rows, H * dh] (leading dimension ldq; H a multiple of Hkv, heads h G .. h G + G - 1 read
  * head h of the cache, G = H / Hkv), over the positions up to the row's own if `causal`, otherwise all of the sequence's.  o [rows, H * dh]; lse fp32 [rows, H]
  * (may be null) = log-sum-exp of the scaled scores.  A row that sees no token becomes zeros, its lse minus infinity.  What a row does not see does not
- * change it, a NaN there included.  Scales are positive, as append leaves them.  q and o do not overlap.  scratch_dev: lpk_cache_attention_scratch floats (needs no device; may be 0), 16-byte aligned; contents
+ * change it, a NaN there included.  Scores, largest scores and sums are of 32 bits.  Weights stand before the values with 24 bits if dtype is fp32; in bf16 they are
+ * rounded, to 2^-16 of a weight where T H / Hkv is 32 or less, otherwise to 2^-12 of it or 2^-24 of the row's largest, whichever is more.  Numbers of q, and of pages with their
+ * scale, that are neither zero nor within 2^-80 .. 2^80 may be beyond what 32 bits hold in between.  Scales are positive, as append leaves them.  q and o do not overlap.
+ * scratch_dev: lpk_cache_attention_scratch floats (needs no device; may be 0), 16-byte aligned; contents
  * undefined on return, so that calls which share it are ordered. */
 int lpk_cache_append(int dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, int rows, const int32_t* starts, const int32_t* lens,
                      const int32_t* table, void* kpages, void* vpages, float* kscale, float* vscale, int B, int T, int Hkv, int dh, int page,

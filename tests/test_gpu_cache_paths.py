@@ -32,10 +32,10 @@ def test_largest_scores_of_the_last_columns(K, dtype, T, page, dh):  # noqa: F81
 
 
 # ------------------------------------------------------------------------------------------------ small weights, small values
-def near_of_their_own(c, o, q):
+def near_of_their_own(c, o, q, causal=0):
     """Every column by what stands in it.  One rounding of the output; a weight as in test_gpu_cache (in 24 bits in fp32, 2^-16 in bf16, 2^-12 with many rows) and in bf16 with many
     rows, whose weights end at 2^-32 of a reference that is 2^8 times the row's largest at most, 2^-24 of that for each token: of its |v|, whatever stands in other columns."""
-    ref, _, size, mass = C.attention(q.astype(np.float64).reshape(c.rows, c.Hkv, c.dh), c.kp, c.vp, c.ks, c.vs, c.seqs(), c.table, False)
+    ref, _, size, mass = C.attention(q.astype(np.float64).reshape(c.rows, c.Hkv, c.dh), c.kp, c.vp, c.ks, c.vs, c.seqs(), c.table, causal)
     n, many, new = int(c.lens[0]), c.T > 32, int(c.starts[1])
     v = np.abs(c.vp * c.vs[..., None, None])[c.table[0]]                     # [pages, heads, dh, page]
     total = v.sum((0, 3)) if many and c.dtype else 0.0
@@ -153,3 +153,19 @@ def test_single_tokens_beside_a_chunk(K, dtype, B, chunk, most):  # noqa: F811
     o, lse, q, _ = attend(K, c, 2)
     right(c, 2, 1, o, lse, q)
     assert c.guards_stand()
+
+
+# ------------------------------------------------------------------------------------------------ the ends of the range
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("T,lens", [(1, 300), (20, 300), (130, 300), (1, 3000), (130, 3000)])
+@pytest.mark.parametrize("of_q,of_k", [(71, -71), (-71, 71), (0, 0)])
+@pytest.mark.parametrize("of_v", [-68, 68])
+def test_ends_of_the_range(K, dtype, T, lens, of_q, of_k, of_v):  # noqa: F811
+    """Queries, keys and values as large and as small as the header allows."""
+    c = Cache(dtype, 31, [T], [lens], 1, 64, 64)
+    c.ks, c.vs = c.ks * 2.0 ** of_k, c.vs * 2.0 ** of_v
+    c.vp[c.vp == 0] = 1.0
+    c.load()
+    o, lse, q, _ = attend(K, c, 1, q=c.rnd(c.rows, 64) * np.float32(2.0 ** of_q))
+    right(c, 1, 1, o, lse, q)
+    near_of_their_own(c, o, q, 1)
