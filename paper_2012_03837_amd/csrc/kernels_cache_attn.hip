@@ -513,7 +513,7 @@ __global__ void __launch_bounds__(64 * W, ND * NC <= 2 ? 2 : 1) k_cache_attn(Cac
 
 // ------------------------------------------------------------------------------------------------ many rows
 // The same for calls with many columns (prompts, chunks of them): a block has 128 columns, a wave 32 of them, and tiles of 64
-// tokens go through LDS, as numbers, for all its waves: keys in bf16, values in f16, each code converted once.  Products are 32 x 32 x 16; the rows of K are dealt
+// tokens go through LDS, as numbers, for all its waves: keys in bf16, values in f16 (bf16 in fp32 calls), each code converted once.  Products are 32 x 32 x 16; the rows of K are dealt
 // to tokens so that a lane's eight scores, and its operand of the second product, are eight tokens in order (token_of).
 // In fp32 weights enter the second product in three bf16 parts, all their 24 bits; in bf16 in f16, whose eleven bits leave 2^-12 of a weight, a sixteenth of the output's own rounding: codes of 8 bits are f16 numbers too.  Neither
 // has room for a weight times any scale of its values, so that they are held relative to the largest such product that the row has met (`top`), at 2^7 of which one stands; both it
